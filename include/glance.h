@@ -43,7 +43,7 @@ enum {
     GLANCE_E_CUDA = -4,        /* a CUDA runtime call failed */
     GLANCE_E_TIMEOUT = -5,     /* a bounded device-side wait gave up */
     GLANCE_E_BOUNDS = -6,      /* device-side index check failed */
-    GLANCE_E_STATE = -7        /* calls out of order (glance_profile_read before glance_profile_enable) */
+    GLANCE_E_STATE = -7        /* calls out of order (glance_profile_read before glance_profile_enable, packing without a pool) */
 };
 
 typedef struct glance_ctx glance_ctx;
@@ -113,6 +113,20 @@ typedef struct {
     uint64_t *anc;                          /* [batch][N][(N+63)/64] */
     int32_t *n_nodes;                       /* [batch] */
 } glance_tree;
+
+/* A cache whose finished pages are held in 4 bits.  16 values along the head dimension share a scale s, the e4m3 value
+ * nearest to max|x| / 6 (448 at most, 0 where that rounds to 0); a value is held as the e2m1 value (0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives) nearest to x / s and stands for s times it; ties go to the even code.  That product is exact in bf16.
+ * 16 values with an infinity or a NaN among them are held as NaN.  4.5 bits a value: 3.56 times less than bf16.
+ * Positions [0, len[s]) of sequence s, whole pages, are read from `pool` in every target layer, later ones from kv_pool, whose
+ * pages below len[s] are then not read by any pass (their entries in glance_seqs.page_table may name any page of the pool).
+ * Only positions below seq_len are read here: of len[s], whole pages of it.  The block head's cache stays in bf16. */
+typedef struct {
+    int32_t n_pages;           /* pages in the pool (per layer) */
+    int32_t *len;              /* device [max_batch]: positions held in 4 bits, multiples of page_size; 0 at the start */
+    const int32_t *page_table; /* device [max_batch][max_pages_per_seq]: page of the pool that holds a sequence's page */
+    void *pool;                /* device, 16-byte aligned, glance_packed_bytes(cfg, n_pages) bytes: (layer, page, kv_head) tiles */
+} glance_packed;
 
 const char *glance_status_string(int32_t status);
 
@@ -198,6 +212,47 @@ int32_t glance_accept_commit(glance_ctx *ctx, const glance_seqs *seqs, const gla
  * path [batch][block_B] (device), path_len [batch] = a+1 (device), new_root [batch] (device). */
 int32_t glance_commit_forced(glance_ctx *ctx, const glance_seqs *seqs, const void *hidden,
                              const int32_t *path, const int32_t *path_len, const int32_t *new_root);
+
+/* Sliding window with first tokens that stay visible, for the target's own passes (prefill, verify): layer l's rows at
+ * position a see position p only if p < sinks or a - p < window[l]; window[l] = 0 is no limit.  `window` is a HOST array of
+ * n_layers entries (read during the call), or NULL for no limit anywhere, as at the start; window[l] >= 0, sinks >= 0.  The
+ * block head is not concerned.  A node's position is seq_len + depth.  Cache pages that no later row can see (whole pages
+ * between the sinks and the window) are not read: their page-table entries are not looked at.  Host call; takes effect from
+ * the next enqueued pass (a captured CUDA graph keeps the setting it was captured with). */
+int32_t glance_set_window(glance_ctx *ctx, const int32_t *window, int32_t sinks);
+
+/* Bytes of a 4-bit pool of n_pages pages a layer (0 if the configuration is unsupported or n_pages < 1). */
+size_t glance_packed_bytes(const glance_config *cfg, int32_t n_pages);
+
+/* Registers a 4-bit pool: from the next enqueued pass on the target's layers read positions below packed->len from it.  The
+ * struct is copied; its device memory stays borrowed.  NULL: everything is read from kv_pool again (unpack first).  While a
+ * pool is registered glance_seq_truncate lowers len[seq] to whole pages of new_len; a caller who lowers seq_len by other means
+ * lowers len too.  Host call. */
+int32_t glance_set_packed(glance_ctx *ctx, const glance_packed *packed);
+
+/* Moves finished pages of every sequence and target layer from kv_pool into the registered 4-bit pool: len[s] rises to
+ * max(0, seq_len[s] - keep) rounded down to whole pages (and never falls here).  keep >= 0 positions at least stay in bf16.
+ * The bf16 pages are left as they are.  GLANCE_E_STATE without a registered pool. */
+int32_t glance_pack_cache(glance_ctx *ctx, const glance_seqs *seqs, int32_t keep);
+
+/* The way back: len[s] falls to new_len[s] rounded down to whole pages (device [batch]; larger values change nothing), and
+ * the values that the pages from there on stand for are written to the pages of seqs->kv_pool.  Before a truncation into the
+ * 4-bit part, or to look at what is held (with a kv_pool of the caller's own in *seqs).  GLANCE_E_STATE without a pool. */
+int32_t glance_unpack_cache(glance_ctx *ctx, const glance_seqs *seqs, const int32_t *new_len);
+
+/* The attention of a target layer's pass over the paged cache, by itself: T rows of each sequence, q (device [batch*T][Hq*d]
+ * bf16, 16-byte aligned) against cache rows 0..seq_len+T-1 of target layer `layer`, softmax scale 1/sqrt(d).  Row i's own key
+ * and value lie at cache row seq_len + i (glance_attention does not write them).  Which of the rows seq_len.. row i sees:
+ * with anc (device [batch][T][(T+63)/64], as in glance_tree) those of its set, and it stands at seq_len + depth, depth being
+ * the number of nodes in its set without itself; causal != 0: rows 0..i (a chain: prefill; anc must be NULL), neither: all T rows
+ * (a block).  In a chain or a block row i stands at seq_len + i.  window and sinks limit all of them as in glance_set_window
+ * (whose setting does not apply here; within a set the distance of two nodes is the number of its nodes behind the nearer
+ * one), and positions held in 4 bits are read from the registered pool.  A row that sees nothing gets zeros.  Cache places
+ * that no row sees may hold anything.  T <= 128 with anc or as a block; a chain may be as long as the page table allows.
+ * seq_len[s] + T positions have to fit the page table and its entries the pools: GLANCE_E_BOUNDS in the status word otherwise,
+ * and that sequence's rows are undefined.  q_lo and out_lo: second bf16 terms as in glance_debug_attention, or NULL. */
+int32_t glance_attention(glance_ctx *ctx, const glance_seqs *seqs, int32_t layer, const void *q, const void *q_lo,
+                         const uint64_t *anc, int32_t T, int32_t causal, int32_t window, int32_t sinks, void *out, void *out_lo);
 
 /* Synchronises the stream and returns the device status word (GLANCE_OK or the first fault);
  * the word is cleared. */

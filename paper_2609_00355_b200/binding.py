@@ -21,6 +21,7 @@ EXPORTS = [
     "glance_accept_commit", "glance_commit_forced", "glance_poll_status", "glance_launch_count",
     "glance_debug_attention", "glance_debug_gemm", "glance_debug_gemm_wide", "glance_profile_enable", "glance_profile_read",
     "glance_topk_static", "glance_debug_trace", "glance_debug_attention_terms", "glance_debug_stall_next_gemm",
+    "glance_set_window", "glance_packed_bytes", "glance_set_packed", "glance_pack_cache", "glance_unpack_cache", "glance_attention",
 ]
 
 
@@ -53,6 +54,10 @@ class Seqs(C.Structure):
     _fields_ = [("batch", C.c_int32), ("n_pages", C.c_int32), ("seq_len", C.c_void_p), ("root", C.c_void_p),
                 ("page_table", C.c_void_p), ("kv_pool", C.c_void_p), ("head_kv_pool", C.c_void_p),
                 ("feat", C.c_void_p), ("feat_count", C.c_void_p)]
+
+
+class Packed(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("len", C.c_void_p), ("page_table", C.c_void_p), ("pool", C.c_void_p)]
 
 
 class Tree(C.Structure):
@@ -123,6 +128,19 @@ def load_library() -> C.CDLL:
     lib.glance_topk_static.restype = C.c_int32
     lib.glance_topk_static.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
                                        C.c_void_p]
+    lib.glance_set_window.restype = C.c_int32
+    lib.glance_set_window.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.c_int32]
+    lib.glance_packed_bytes.restype = C.c_size_t
+    lib.glance_packed_bytes.argtypes = [C.POINTER(Config), C.c_int32]
+    lib.glance_set_packed.restype = C.c_int32
+    lib.glance_set_packed.argtypes = [C.c_void_p, C.POINTER(Packed)]
+    lib.glance_pack_cache.restype = C.c_int32
+    lib.glance_pack_cache.argtypes = [C.c_void_p, C.POINTER(Seqs), C.c_int32]
+    lib.glance_unpack_cache.restype = C.c_int32
+    lib.glance_unpack_cache.argtypes = [C.c_void_p, C.POINTER(Seqs), C.c_void_p]
+    lib.glance_attention.restype = C.c_int32
+    lib.glance_attention.argtypes = [C.c_void_p, C.POINTER(Seqs), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                     C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
     lib.glance_launch_count.restype = C.c_int64
     lib.glance_launch_count.argtypes = [C.c_void_p]
     _lib = lib
@@ -176,6 +194,25 @@ class TreeBuffers:
         self.n_nodes = torch.ones(batch, **i32)
         self.c = Tree(*[_ptr(t) for t in (self.token, self.parent, self.depth, self.rank, self.score, self.anc,
                                           self.n_nodes)])
+
+
+class PackedCache:
+    """Device memory of a 4-bit pool for an engine's target layers, laid out as glance_packed expects.
+
+    `n_pages` pages (a layer), as many as the engine's own pool by default, handed out in order; a caller with an allocator of
+    its own writes `page_table` instead.
+    """
+
+    def __init__(self, eng: "Engine", n_pages: Optional[int] = None):
+        self.n_pages = eng.n_pages if n_pages is None else n_pages
+        nbytes = eng.lib.glance_packed_bytes(C.byref(eng.ccfg), self.n_pages)
+        if nbytes == 0:
+            raise GlanceError("a 4-bit pool needs at least one page")
+        self.len = torch.zeros(eng.batch, dtype=torch.int32, device=eng.device)
+        ids = torch.arange(eng.batch * eng.pages_per_seq, dtype=torch.int32, device=eng.device).view(eng.batch, -1)
+        self.page_table = torch.where(ids < self.n_pages, ids, -1)
+        self.pool = torch.zeros(nbytes, dtype=torch.uint8, device=eng.device)
+        self.c = Packed(self.n_pages, _ptr(self.len), _ptr(self.page_table), _ptr(self.pool))
 
 
 class Engine:
@@ -315,6 +352,43 @@ class Engine:
         v = C.c_int32(0)
         _check(self.lib.glance_poll_status(self.ctx, C.byref(v)), "glance_poll_status")
         return v.value
+
+    def glance_set_window(self, window: Optional[Sequence[int]] = None, sinks: int = 0):
+        """window: one value a target layer (0 = no limit), or None for no limit anywhere."""
+        if window is not None and len(window) != self.cfg.n_layers:
+            raise GlanceError("glance_set_window: one window a target layer")
+        arr = None if window is None else (C.c_int32 * len(window))(*window)
+        _check(self.lib.glance_set_window(self.ctx, arr, sinks), "glance_set_window")
+
+    def glance_set_packed(self, packed: Optional[PackedCache]):
+        """Registers (and keeps alive) a 4-bit pool for the target's layers, or goes back to the bf16 pool alone."""
+        _check(self.lib.glance_set_packed(self.ctx, None if packed is None else C.byref(packed.c)), "glance_set_packed")
+        self.packed = packed
+
+    def glance_pack_cache(self, keep: int = 0):
+        """Finished pages into the 4-bit pool; the last `keep` positions at least stay in bf16."""
+        _check(self.lib.glance_pack_cache(self.ctx, C.byref(self.seqs), keep), "glance_pack_cache")
+
+    def glance_unpack_cache(self, new_len: torch.Tensor, kv_pool: Optional[torch.Tensor] = None):
+        """Pages from new_len [batch] (int32, device) on back to bf16: into the engine's pool, or into another of its shape."""
+        assert new_len.dtype == torch.int32 and new_len.numel() == self.batch
+        seqs = self.seqs
+        if kv_pool is not None:
+            assert kv_pool.shape == self.kv_pool.shape and kv_pool.dtype == self.kv_pool.dtype
+            seqs = Seqs.from_buffer_copy(self.seqs)
+            seqs.kv_pool = _ptr(kv_pool)
+        _check(self.lib.glance_unpack_cache(self.ctx, C.byref(seqs), _ptr(new_len)), "glance_unpack_cache")
+
+    def glance_attention(self, layer: int, q: torch.Tensor, T: int, out: torch.Tensor, anc: Optional[torch.Tensor] = None,
+                         causal: bool = False, window: int = 0, sinks: int = 0, q_lo: Optional[torch.Tensor] = None,
+                         out_lo: Optional[torch.Tensor] = None):
+        """Attention of T rows a sequence over layer `layer`'s cache (window, sinks, 4-bit pages): see glance.h."""
+        shape = self.batch * T * self.cfg.n_q_heads * self.cfg.head_dim
+        for x in (q, out, q_lo, out_lo):
+            assert x is None or (x.dtype == torch.bfloat16 and x.numel() == shape), "bf16 tensors of batch * T rows"
+        assert anc is None or (anc.dtype == torch.int64 and anc.numel() == self.batch * T * ((T + 63) // 64)), "anc: 64-bit words"
+        _check(self.lib.glance_attention(self.ctx, C.byref(self.seqs), layer, _ptr(q), _ptr(q_lo), _ptr(anc), T, 1 if causal else 0,
+                                         window, sinks, _ptr(out), _ptr(out_lo)), "glance_attention")
 
     def glance_debug_attention(self, layer: int, q: torch.Tensor, anc: Optional[torch.Tensor], T: int, out: torch.Tensor,
                                q_lo: Optional[torch.Tensor] = None, out_lo: Optional[torch.Tensor] = None):

@@ -30,7 +30,16 @@
 // The key splits of a tile form a thread-block cluster and are merged through distributed shared memory
 // (one asynchronous bulk copy per owner CTA, byte-counted on the owner's mbarrier).  Every mbarrier wait is
 // bounded; a wait that gives up records GLANCE_E_TIMEOUT.
+//
+// A cache that is not read whole (template parameter CACHE; the pass without it is compiled as if it were not there):
+// kWindow: a tile's pages are the entries of a list (packed.cuh), so a tile's halves need not be neighbours; a row sees the
+//   keys below `sinks`, those from its window's start on, and what is left of its ancestor set.  Rows of V that no row of
+//   the tile sees (a page's rest before the window, behind the sinks or behind the last key) are zeroed by a helper warp.
+// kHeld: pages below held_len come from the 4-bit pool.  One bulk copy brings a page's K or V codes into a ring of
+//   three raw tiles, four helper warps convert them (exactly) to bf16 in the operand tile, next to the halves that the tensor
+//   copies bring, so everything after that is the same.  An operand tile is then full when the copies and all four warps are.
 #include "kernels.cuh"
+#include "packed.cuh"
 #include "tc_ptx.cuh"
 
 namespace glance {
@@ -54,7 +63,10 @@ constexpr int CK = 32;                   // keys whose scores and probabilities 
 constexpr int P_TERMS = 2;               // bf16 terms of a probability
 constexpr int NSOFT = 128 * NG;          // softmax / epilogue threads: one per row and group
 constexpr int ECG = NG;                  // column groups of the epilogue: a row's d outputs are split over them
-constexpr int NTHREADS = 64 + NSOFT;
+enum { kWhole = 0, kWindow = 1, kHeld = 2 };                 // CACHE
+constexpr int n_helpers(int cache) { return cache == kHeld ? 4 : cache == kWindow ? 1 : 0; }       // warps behind the softmax warps
+constexpr int n_threads(int cache) { return 64 + NSOFT + 32 * n_helpers(cache); }
+constexpr int RAW = 3;                   // raw 4-bit tiles (K or V of 128 keys) in flight
 static_assert(CK == 32, "the visibility bit set of 32 keys is one word");
 
 // 16 accumulator columns of a row, combined over the softmax groups: sum_g w[g] * O_g.  Warp-collective.  Only the
@@ -93,6 +105,11 @@ struct Smem {
     // d 64 would fit twice into an SM's shared memory, and clusters whose CTAs hold the columns crosswise would wait for each
     // other in a cluster barrier
     static constexpr int TOTAL = OPER_BYTES + 1024 > (int)least_smem(TMEM_COLS) ? OPER_BYTES + 1024 : (int)least_smem(TMEM_COLS);
+    static constexpr int RAW_BYTES = 2 * packed::Tile<D>::HALF;          // K or V of two pages
+    static constexpr int total(int cache) {
+        const int need = OPER_BYTES + 1024 + (cache == kHeld ? RAW * RAW_BYTES : 0);
+        return need > TOTAL ? need : TOTAL;
+    }
     static_assert(O_COL + NG * D <= TMEM_COLS, "tensor memory budget");
     static_assert(RECV_AT + RECV_BYTES <= OPER_BYTES, "the merge fits the operand buffers");
     static_assert(RECV_AT % 16 == 0 && ROWF % 4 == 0, "bulk copies start on 16-byte boundaries");
@@ -100,12 +117,13 @@ struct Smem {
 
 struct alignas(8) AttnBars {
     uint64_t q_ready, k_full[NG], k_empty[NG], v_full[NG], v_empty[NG], s_full[NG], p_full[NG], all_done, v_zero, merge;
+    uint64_t raw_full[RAW], raw_empty[RAW];              // kHeld
     uint32_t tmem_base;
     int abort_flag;
 };
 
-template <int D>
-__global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_constant__ CUtensorMap map_kv, AttnParams p) {
+template <int D, int CACHE>
+__global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __grid_constant__ CUtensorMap map_kv, AttnParams p) {
     constexpr int SLABS = Smem<D>::SLABS, SLAB = Smem<D>::SLAB, KV_BYTES = Smem<D>::KV_BYTES;
     constexpr int CH = D / 8;                            // 16-byte chunks per row
     extern __shared__ unsigned char smem_raw[];
@@ -113,6 +131,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
     unsigned char *sQ = smem;                                        // hi plane, lo plane
     unsigned char *sK = sQ + Smem<D>::Q_BYTES;                       // tiles [slab][128 keys][128 bytes], one per group
     unsigned char *sV = sK + NG * KV_BYTES;
+    unsigned char *sRaw = sV + NG * KV_BYTES;                        // kHeld: raw tiles
     __shared__ AttnBars bars;
     __shared__ float red_m[NG][QT], red_l[NG][QT];        // the groups' reference maxima and row sums
 
@@ -135,9 +154,9 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
     if (threadIdx.x == 0) {
         mbar_init(&bars.q_ready, NSOFT / 32);            // one arrival per softmax warp
         for (int b = 0; b < NG; ++b) {
-            mbar_init(&bars.k_full[b], 1);
+            mbar_init(&bars.k_full[b], CACHE == kHeld ? 5 : 1);       // the copies, and one arrival per helper warp
             mbar_init(&bars.k_empty[b], 1);
-            mbar_init(&bars.v_full[b], 1);
+            mbar_init(&bars.v_full[b], CACHE == kHeld ? 5 : 1);
             mbar_init(&bars.v_empty[b], 1);
             mbar_init(&bars.s_full[b], 1);
             mbar_init(&bars.p_full[b], 4);               // one arrival per warp of the group
@@ -145,6 +164,12 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
         mbar_init(&bars.all_done, 1);
         mbar_init(&bars.v_zero, 1);
         mbar_init(&bars.merge, 1);
+        if constexpr (CACHE == kHeld) {
+            for (int b = 0; b < RAW; ++b) {
+                mbar_init(&bars.raw_full[b], 1);
+                mbar_init(&bars.raw_empty[b], 4);        // one arrival per helper warp
+            }
+        }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (p.S > 1) {
@@ -171,16 +196,32 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
     // launched without programmatic overlap and releases none of its dependents early.  So both may be read before the
     // dependency wait.  Pages entirely below seq_len - block_B hold committed
     // context that no kernel of this pass writes, so the producer prefetches them before the wait as well.
-    const int P = p.seq_len[s];
+    const int P = CACHE ? max(p.seq_len[s], 0) : p.seq_len[s];
     // keys any row of this tile sees: all of them, or, in a chain, those up to the tile's last node
     const int n_keys = P + (p.causal ? (min((qt + 1) * QT, PR) - 1) / G + 1 : p.T);
-    const int n_pages = (n_keys + kPage - 1) / kPage;
+    // the pages that any row of this tile sees: all, or (CACHE) the entries of a list
+    const int node_first = p.causal ? qt * QT / G : 0, node_last = p.causal ? (min((qt + 1) * QT, PR) - 1) / G : p.T - 1;
+    const int low_min = CACHE ? window_low(P + node_first, p.window) : 0, low_max = CACHE ? window_low(P + node_last, p.window) : 0;
+    PageList list{0, 0, (n_keys + kPage - 1) / kPage};
+    if constexpr (CACHE != kWhole) list = page_list(n_keys, low_min, p.sinks);
+    const int n_pages = list.count;
+    const int held = CACHE == kHeld ? min(max(p.held_len[s], 0), P) / kPage : 0;      // pages below this one come from the 4-bit pool
     // ceil-distribution of pages: the extra ones go to the first splits, because the last split already carries the
     // costlier masked tiles and the partial page
     const int pg_begin = (int)(((long long)split * n_pages + p.S - 1) / p.S);
     const int pg_end = (int)(((long long)(split + 1) * n_pages + p.S - 1) / p.S);
     const int np = pg_end - pg_begin;                    // pages of this CTA
     const int nt = (np + 1) / 2;                         // tiles, the last one may have one page only
+    // half h of tile i: its page, and (kHeld) whether that is held in 4 bits
+    auto page_of = [&](int i, int h) { return CACHE ? list.page(pg_begin + 2 * i + h) : pg_begin + 2 * i + h; };
+    // CACHE: rows [lo, hi) of a page that some row of the tile may see are a prefix (sinks, last key), a suffix (window), or all
+    auto unseen = [&](int pg, int r) {
+        const int key = pg * kPage + r;
+        return key >= n_keys || (key >= p.sinks && key < low_min);
+    };
+    auto has_unseen = [&](int pg) { return unseen(pg, 0) || unseen(pg, kPage - 1) || ((pg + 1) * kPage > p.sinks && pg * kPage < p.sinks && p.sinks < low_min); };
+    // tiles whose V has rows to zero before its second MMA (by a helper warp)
+    auto needs_zeros = [&](int i) { return has_unseen(page_of(i, 0)) || (np - 2 * i > 1 && has_unseen(page_of(i, 1))); };
     const int32_t *pt = p.page_table + (size_t)s * p.geom.max_pages_per_seq;
     // second terms of queries / probabilities on pure-context tiles (see AttnParams::lo_skip)
     const bool skip_q_lo = (p.lo_skip & 1) && P >= p.lo_skip_min_keys;
@@ -201,9 +242,16 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
             // so they may be fetched before the dependency wait.
             auto load_tile = [&](int i, int kv, unsigned char *dst, uint64_t *bar) {
                 const int pages = min(2, np - 2 * i);
-                mbar_expect_tx(bar, (uint32_t)(pages * (KV_BYTES / 2)));
+                int copied = pages;
+                if constexpr (CACHE == kHeld) {
+                    copied = 0;
+                    for (int h = 0; h < pages; ++h) copied += page_of(i, h) >= held ? 1 : 0;
+                }
+                if (copied) mbar_expect_tx(bar, (uint32_t)(copied * (KV_BYTES / 2)));
+                else mbar_arrive(bar);
                 for (int h = 0; h < pages; ++h) {
-                    const int pg = pg_begin + 2 * i + h;
+                    const int pg = page_of(i, h);
+                    if (CACHE == kHeld && pg < held) continue;
                     if (!waited && (pg + 1) * kPage > P - kMaxBlock) {
                         pdl_wait();
                         waited = true;
@@ -221,8 +269,41 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
             // K and V tiles advance independently, each as far ahead as its ring allows: one thread polls both rings
             uint64_t stall_t0 = 0;
             uint32_t spins = 0;
-            while (issued_k < nt || issued_v < nt) {
+            // kHeld: raw tiles in the order K, V of tile 0, K, V of tile 1, ..; a tile without held pages takes no slot
+            int raw_job = CACHE == kHeld ? 0 : 2 * nt, raw_used = 0;
+            while (issued_k < nt || issued_v < nt || raw_job < 2 * nt) {
                 bool progressed = false;
+                if constexpr (CACHE == kHeld) {
+                    if (raw_job < 2 * nt) {
+                        const int i = raw_job >> 1, kv = raw_job & 1, pages = min(2, np - 2 * i);
+                        int n = 0;
+                        for (int h = 0; h < pages; ++h) n += page_of(i, h) < held ? 1 : 0;
+                        const int slot = raw_used % RAW;
+                        if (n == 0) {
+                            ++raw_job;
+                            progressed = true;
+                        } else if (mbar_try_wait(&bars.raw_empty[slot], ((uint32_t)(raw_used / RAW) & 1u) ^ 1u)) {
+                            constexpr int HALF = packed::Tile<D>::HALF;
+                            mbar_expect_tx(&bars.raw_full[slot], (uint32_t)(n * HALF));
+                            for (int h = 0; h < pages; ++h) {
+                                const int pg = page_of(i, h);
+                                if (pg >= held) continue;
+                                int page = pg < p.geom.max_pages_per_seq ? p.held_table[(size_t)s * p.geom.max_pages_per_seq + pg] : -1;
+                                if (page < 0 || page >= p.held_pages) {
+                                    page = 0;
+                                    set_status(p.status, GLANCE_E_BOUNDS);
+                                }
+                                const unsigned char *src = p.held_layer + ((size_t)page * p.Hkv + kvh) * packed::Tile<D>::BYTES + kv * HALF;
+                                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                             ::"r"(smem_u32(sRaw + slot * Smem<D>::RAW_BYTES + h * HALF)), "l"(src), "r"((uint32_t)HALF),
+                                               "r"(smem_u32(&bars.raw_full[slot])) : "memory");
+                            }
+                            ++raw_used;
+                            ++raw_job;
+                            progressed = true;
+                        }
+                    }
+                }
                 const int ks = issued_k & 1, vs = issued_v & 1;
                 if (issued_k < nt && mbar_try_wait(&bars.k_empty[ks], ((uint32_t)(issued_k >> 1) & 1u) ^ 1u)) {
                     load_tile(issued_k, 0, sK + ks * KV_BYTES, &bars.k_full[ks]);
@@ -249,13 +330,21 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
                 }
             }
             if (!waited) pdl_wait();
+            if constexpr (CACHE == kHeld) {
+                if (*abort_flag)                         // raw copies already issued must land, too
+                    for (int i = max(0, raw_used - RAW); i < raw_used; ++i) {
+                        const uint64_t t0 = global_ns();
+                        while (!mbar_try_wait(&bars.raw_full[i % RAW], (uint32_t)(i / RAW) & 1u))
+                            if (global_ns() - t0 > kWaitLimitNs) break;
+                    }
+            }
         }
         // The page that holds the last key may continue with rows that belong to nobody (any bits, NaN included):
         // this warp zeroes them in the V tile once it has landed, and tells the MMA issuer.  The wait is exact:
         // this thread issued the copy, and no later copy can follow into the slot before that tile's second MMA.
         const int last_valid = n_keys - (pg_begin + 2 * (nt - 1)) * kPage;      // keys of this CTA's last tile
         const int last_rows = (np - 2 * (nt - 1)) * kPage;                      // rows of the pages that it has
-        if (nt > 0 && last_valid < last_rows) {
+        if (!CACHE && nt > 0 && last_valid < last_rows) {
             const int i = nt - 1, slot = i & 1;
             int got = 0;
             if (lane == 0) got = (issued_v == nt && mbar_wait(&bars.v_full[slot], (uint32_t)(i >> 1) & 1u, abort_flag, p.status)) ? 1 : 0;
@@ -294,7 +383,8 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
             const uint32_t idesc_o = umma_idesc_bmn(D);           // M 128, N d, B = V is MN-major
             const int planes = p.q_lo ? 2 : 1;
             auto pages_of = [&](int i) { return min(2, np - 2 * i); };
-            auto in_context = [&](int i) { return (pg_begin + 2 * i + pages_of(i)) * kPage <= P; };
+            auto in_context = [&](int i) { return (CACHE ? (page_of(i, pages_of(i) - 1) + 1) : pg_begin + 2 * i + pages_of(i)) * kPage <= P; };
+            int zeroed = 0;                              // CACHE: tiles that waited for a helper's zeros
             auto issue_s = [&](int i) -> bool {
                 const int b = i & 1;
                 const int planes_i = (skip_q_lo && in_context(i)) ? 1 : planes;
@@ -323,7 +413,12 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
                 const uint32_t ph = (uint32_t)(i >> 1) & 1u;
                 if (!mbar_wait(&bars.v_full[b], ph, abort_flag, p.status)) { ok = false; break; }
                 // the rows after the last key have been zeroed by the producer warp
-                if (i == nt - 1 && n_keys < pg_end * kPage && !mbar_wait(&bars.v_zero, 0, abort_flag, p.status)) { ok = false; break; }
+                if constexpr (CACHE != kWhole) {
+                    if (needs_zeros(i)) {
+                        if (!mbar_wait(&bars.v_zero, (uint32_t)zeroed & 1u, abort_flag, p.status)) { ok = false; break; }
+                        ++zeroed;
+                    }
+                } else if (i == nt - 1 && n_keys < pg_end * kPage && !mbar_wait(&bars.v_zero, 0, abort_flag, p.status)) { ok = false; break; }
                 if (!mbar_wait(&bars.p_full[b], ph, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t vbase = smem_u32(sV + b * KV_BYTES);
@@ -341,6 +436,92 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
                 if (i + NG < nt && !issue_s(i + NG)) { ok = false; break; }
             }
             if (ok) umma_commit(&bars.all_done);         // every MMA of this CTA has completed when this barrier flips
+        }
+        __syncwarp();
+    } else if (CACHE != kWhole && warp >= 2 + NSOFT / 32) {
+        // ---------------- helper warps: 4-bit tiles -> bf16 operand tiles, zeros in rows of V that nobody sees ----------------
+        const int helper = warp - 2 - NSOFT / 32;
+        int raw_used = 0;
+        bool ok = true;
+        for (int i = 0; i < nt && ok; ++i) {
+            const int b = i & 1, pages = min(2, np - 2 * i);
+            const uint32_t ph = (uint32_t)(i >> 1) & 1u;
+            if constexpr (CACHE == kWindow) {
+                // every phase of the slot is seen, so that the wait for a tile below cannot take an older one for it
+                ok = mbar_wait(&bars.v_empty[b], ph ^ 1u, abort_flag, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+            }
+            if constexpr (CACHE == kHeld) {
+                constexpr int HALF = packed::Tile<D>::HALF, GROUPS = packed::Tile<D>::GROUPS;
+                for (int kv = 0; kv < 2 && ok; ++kv) {
+                    const bool h0 = page_of(i, 0) < held, h1 = pages > 1 && page_of(i, 1) < held;
+                    uint64_t *full = kv ? &bars.v_full[b] : &bars.k_full[b];
+                    if (h0 || h1) {
+                        const int slot = raw_used % RAW;
+                        ok = mbar_wait(kv ? &bars.v_empty[b] : &bars.k_empty[b], ph ^ 1u, abort_flag, p.status) &&
+                             mbar_wait(&bars.raw_full[slot], (uint32_t)(raw_used / RAW) & 1u, abort_flag, p.status);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        const unsigned char *raw = sRaw + slot * Smem<D>::RAW_BYTES;
+                        unsigned char *dst = (kv ? sV : sK) + b * KV_BYTES;
+                        // a thread converts one group of 16: 8 bytes of codes and a scale -> two 16-byte pieces of the key's row
+#pragma unroll 2
+                        for (int it = helper * 32 + lane; it < 2 * kPage * GROUPS; it += 128) {
+                            const int h = it / (kPage * GROUPS), key = it / GROUPS % kPage, c = it % GROUPS;
+                            if (!(h ? h1 : h0)) continue;
+                            const uint2 w = *reinterpret_cast<const uint2 *>(raw + h * HALF + packed::code_at<D>(key, c >> 1) + (c & 1) * 8);
+                            const uint32_t sc = raw[h * HALF + packed::Tile<D>::SCALES + key * GROUPS + c];
+                            const uint32_t s2 = packed::scales_to_half(sc | sc << 8);
+                            uint32_t v[2][4];
+                            packed::codes_to_half(w.x, v[0]);
+                            packed::codes_to_half(w.y, v[1]);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                v[0][k] = packed::half2_to_bf16(packed::mul_half2(v[0][k], s2));
+                                v[1][k] = packed::half2_to_bf16(packed::mul_half2(v[1][k], s2));
+                            }
+                            const int row = h * kPage + key;
+                            // lanes of the first slab store their first piece while the second slab's store their second: no bank twice
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int second = SLABS > 1 ? k ^ (c >> 2) : k, ch = 2 * c + second;
+                                const uint4 o = second ? make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]) : make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
+                                *reinterpret_cast<uint4 *>(dst + (ch >> 3) * SLAB + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = o;
+                            }
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars.raw_empty[slot]);
+                        ++raw_used;
+                    } else {
+                        // nothing to convert: the arrival must not run ahead of the slot's previous tile
+                        ok = mbar_wait(kv ? &bars.v_empty[b] : &bars.k_empty[b], ph ^ 1u, abort_flag, p.status);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                    }
+                    if (lane == 0) mbar_arrive(full);
+                }
+                if (!ok) break;
+            }
+            if (helper == 0 && needs_zeros(i)) {
+                // the tile has landed; its second MMA waits for this warp
+                ok = mbar_wait(&bars.v_full[b], ph, abort_flag, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                unsigned char *v = sV + b * KV_BYTES;
+                for (int h = 0; h < pages; ++h) {
+                    const int pg = page_of(i, h);
+                    if (!has_unseen(pg)) continue;
+                    for (int it = lane; it < kPage * CH; it += 32) {
+                        const int r = it / CH, c = it % CH, row = h * kPage + r;
+                        if (unseen(pg, r)) *reinterpret_cast<int4 *>(v + (c >> 3) * SLAB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_int4(0, 0, 0, 0);
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.v_zero);
+            }
         }
         __syncwarp();
     } else {
@@ -380,7 +561,13 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
         asm volatile("cp.async.commit_group;" ::);
         // the row's ancestor words travel while the copies are in flight
         uint64_t anc0 = ~0ull, anc1 = ~0ull;               // no mask: every extra key is visible
-        if (p.anc && !p.causal) {
+        int low = 0;                                       // CACHE: the row's window starts here
+        if constexpr (CACHE != kWhole) {
+            const RowSight rs = row_sight(p.anc ? p.anc + (size_t)s * p.T * p.W : nullptr, p.causal, node, p.T, P, p.window, p.sinks);
+            anc0 = rs.bits[0];
+            anc1 = rs.bits[1];
+            low = rs.low;
+        } else if (p.anc && !p.causal) {
             const uint64_t *a = p.anc + ((size_t)s * p.T + node) * p.W;
             anc0 = a[0];
             anc1 = p.W > 1 ? a[1] : 0ull;
@@ -407,7 +594,43 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
             if (!ok) break;                               // a warp that leaves stops arriving at p_full: every wait is bounded
             if (trace && threadIdx.x == 64 && i == 0) trace[4] = global_ns();
             tc_fence_after();
-            if (key0 + pages * kPage > P) {
+            if constexpr (CACHE != kWhole) {
+                // As below, for a list of pages: what a row sees of 32 keys is those before the sinks' end or from its window's
+                // start on, up to its last key; of the new rows, for a tree or block, what is left of its set.
+                auto part_seen = [&](int pg) { return (pg + 1) * kPage > P || ((pg + 1) * kPage > p.sinks && pg * kPage < low_max); };
+#pragma unroll 1
+                for (int c = 0; c < pages * (kPage / CK); ++c) {
+                    const int pg = page_of(i, c / (kPage / CK));
+                    if (!part_seen(pg)) continue;
+                    const int k0 = pg * kPage + c % (kPage / CK) * CK;
+                    auto from = [&](int n) { return n <= 0 ? 0xffffffffu : n >= 32 ? 0u : 0xffffffffu << n; };       // keys k0 + n ..
+                    uint32_t vis = from(low - k0) | ~from(p.sinks - k0);
+                    if (p.causal) {
+                        vis &= ~from(P + node + 1 - k0);
+                    } else {
+                        const uint32_t fresh = from(P - k0);             // of the new rows
+                        const int b0 = k0 - P;
+                        uint32_t ext = 0u;
+                        if (b0 > -32) {
+                            if (b0 < 0) ext = (uint32_t)anc0 << -b0;
+                            else {
+                                const uint64_t lo = b0 >= 128 ? 0ull : b0 >= 64 ? anc1 : anc0, hi = b0 >= 64 ? 0ull : anc1;
+                                const int sh = b0 & 63;
+                                ext = (uint32_t)(sh == 0 ? lo : ((lo >> sh) | (hi << (64 - sh))));
+                            }
+                        }
+                        vis = (vis & ~fresh) | (ext & fresh);
+                    }
+                    if (__all_sync(0xffffffffu, vis == 0xffffffffu)) continue;
+                    uint32_t v[32];
+                    tmem_ld32(tmem_Sg + (uint32_t)(c * CK), v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = ((vis >> j) & 1u) ? v[j] : 0xff800000u;    // -inf
+                    tmem_st32(tmem_Sg + (uint32_t)(c * CK), v);
+                }
+                tmem_st_wait();
+            } else if (key0 + pages * kPage > P) {
                 // Visibility of 32 keys as one bit set: committed keys (< P) are visible, keys past the last one are not,
                 // extra key b is visible if bit b of the row's ancestor set is (all of them without a mask).
                 // b0 = index of the first key among the extra keys; negative inside the context.
@@ -537,7 +760,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
         // ---------------- epilogue ----------------
         constexpr int OC = D / ECG;                       // output columns of a thread
         if (p.S == 1) {
-            const float inv = 1.f / l_row;
+            const float inv = CACHE && l_row == 0.f ? 0.f : 1.f / l_row;      // a row that sees nothing
             const bool aligned = (((uintptr_t)p.out | (uintptr_t)p.out_lo) & 15) == 0;     // (rows start on multiples of 128 bytes)
             const size_t off = ((size_t)(s * p.T + node) * p.Hq + kvh * G + g) * D + grp * OC;
 #pragma unroll 1
@@ -640,12 +863,12 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
                 float den = 0.f;
 #pragma unroll
                 for (int sp = 0; sp < MAX_SPLITS; ++sp) {  // split order: bit-reproducible
-                    const float ws = ex2_approx(ms[sp] - M);   // 2^-inf = 0 for an empty split
+                    const float ws = CACHE && M == -INFINITY ? 0.f : ex2_approx(ms[sp] - M);   // 2^-inf = 0 for an empty split
                     den += ws * ls[sp];
                     acc.x += ws * va[sp].x; acc.y += ws * va[sp].y; acc.z += ws * va[sp].z; acc.w += ws * va[sp].w;
                     bcc.x += ws * vb[sp].x; bcc.y += ws * vb[sp].y; bcc.z += ws * vb[sp].z; bcc.w += ws * vb[sp].w;
                 }
-                const float inv = 1.f / den;
+                const float inv = CACHE && den == 0.f ? 0.f : 1.f / den;
                 const int prr = qt * QT + row_lo + lr;
                 const size_t off = ((size_t)(s * p.T + prr / G) * p.Hq + kvh * G + prr % G) * D;
                 store_two_term(p.out + off + c0, p.out_lo ? p.out_lo + off + c0 : nullptr,
@@ -660,7 +883,7 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
     if (p.trace && threadIdx.x == 64) atomicMax(p.trace + 15, (unsigned long long)global_ns());  // grid span: last end
     if (p.S > 1) {
         __syncwarp();
-        if (warp < 2) {                                  // the two arrivals of the softmax warps' merge
+        if (warp < 2 || (CACHE && warp >= 2 + NSOFT / 32)) {     // the two arrivals of the softmax warps' merge
             cluster_arrive();
             cluster_wait();
             cluster_arrive();
@@ -675,18 +898,18 @@ __global__ void __launch_bounds__(NTHREADS, 1) attn_tc_kernel(const __grid_const
     }
 }
 
-template <int D>
+template <int D, int CACHE>
 cudaError_t launch_d(const AttnParams &p, const CUtensorMap &map_kv, dim3 grid, cudaStream_t st) {
     static bool once = false;
     if (!once) {
-        cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
+        cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, CACHE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::total(CACHE));
         if (e != cudaSuccess) return e;
         once = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(NTHREADS, 1, 1);
-    cfg.dynamicSmemBytes = Smem<D>::TOTAL;
+    cfg.blockDim = dim3(n_threads(CACHE), 1, 1);
+    cfg.dynamicSmemBytes = Smem<D>::total(CACHE);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -697,18 +920,19 @@ cudaError_t launch_d(const AttnParams &p, const CUtensorMap &map_kv, dim3 grid, 
     attr[1].val.clusterDim.z = p.S;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, attn_tc_kernel<D>, map_kv, p);
+    return cudaLaunchKernelEx(&cfg, attn_tc_kernel<D, CACHE>, map_kv, p);
 }
 
-// largest number of co-resident clusters of `cs` CTAs of this kernel (queried once per cluster size)
+// largest number of co-resident clusters of `cs` CTAs of this kernel (queried once per cluster size; a CTA has the SM to
+// itself with or without CACHE)
 template <int D>
 int max_active_clusters(int cs) {
     static int cache[MAX_SPLITS + 1] = {0};
     if (cache[cs] == 0) {
-        cudaFuncSetAttribute(attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
+        cudaFuncSetAttribute(attn_tc_kernel<D, kWhole>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1, 1, cs);
-        cfg.blockDim = dim3(NTHREADS, 1, 1);
+        cfg.blockDim = dim3(n_threads(kWhole), 1, 1);
         cfg.dynamicSmemBytes = Smem<D>::TOTAL;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -718,7 +942,7 @@ int max_active_clusters(int cs) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D>, &cfg) != cudaSuccess || n < 1) n = 148 / cs - 4;
+        if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kWhole>, &cfg) != cudaSuccess || n < 1) n = 148 / cs - 4;
         cache[cs] = n < 1 ? 1 : n;
     }
     return cache[cs];
@@ -751,8 +975,15 @@ int attention_tc_splits(int T, int G, int Hkv, int batch, int d) {
 cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
     const int G = p.Hq / p.Hkv;
     dim3 grid(attention_tc_q_tiles(p.T, G), p.Hkv, p.batch * p.S);
-    if (p.d == 128) return launch_d<128>(p, map_kv, grid, st);
-    return launch_d<64>(p, map_kv, grid, st);
+    if (p.d == 128) return launch_d<128, kWhole>(p, map_kv, grid, st);
+    return launch_d<64, kWhole>(p, map_kv, grid, st);
+}
+
+cudaError_t launch_attention_cache(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
+    const int G = p.Hq / p.Hkv;
+    dim3 grid(attention_tc_q_tiles(p.T, G), p.Hkv, p.batch * p.S);
+    if (p.held_len) return p.d == 128 ? launch_d<128, kHeld>(p, map_kv, grid, st) : launch_d<64, kHeld>(p, map_kv, grid, st);
+    return p.d == 128 ? launch_d<128, kWindow>(p, map_kv, grid, st) : launch_d<64, kWindow>(p, map_kv, grid, st);
 }
 
 }  // namespace glance

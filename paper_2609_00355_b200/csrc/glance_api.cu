@@ -9,6 +9,7 @@
 
 #include "gemm_tc.cuh"
 #include "kernels.cuh"
+#include "packed.cuh"
 
 using namespace glance;
 
@@ -70,6 +71,9 @@ struct Workspace {
     unsigned long long *tk_cand;   // [vocab tiles][batch*B][kTopkTileCap]
     float *wide_planes;            // partial tiles of gemm_wide_kernel, or nullptr where its rule never chooses it
     int32_t *wide_counters;        // [kWideCut][2], zero between launches
+    float *few_parts, *few_ml;     // attention of few rows: partial results [kFewParts][kFewRows][d] and [..][2]
+    int32_t *few_counters;         // [max_batch * Hkv], zero between launches
+    int32_t *pack_counter;         // zero between launches
     size_t total;
 };
 
@@ -131,6 +135,10 @@ Workspace carve(const glance_config &c, const Dims &d, unsigned char *base) {
     }
     w.wide_planes = wide ? (float *)take(kWidePlaneFloats * 4) : nullptr;
     w.wide_counters = (int32_t *)take((size_t)kWideCut * 2 * 4);
+    w.few_parts = (float *)take((size_t)kFewParts * kFewRows * c.head_dim * 4);
+    w.few_ml = (float *)take((size_t)kFewParts * kFewRows * 2 * 4);
+    w.few_counters = (int32_t *)take((size_t)c.max_batch * c.n_kv_heads * 4);
+    w.pack_counter = (int32_t *)take(4);
     w.total = off;
     return w;
 }
@@ -190,6 +198,10 @@ struct glance_ctx {
     int trace_slots = 0, trace_next = 0;
     // attention: which second bf16 terms the pure-context key tiles drop, and from which context length on
     int attn_lo_skip = 0, attn_lo_min_keys = 0;
+    // what the target's passes see of the cache, and where its finished pages are held in 4 bits
+    std::vector<int32_t> window;      // per target layer, 0 = no limit
+    int sinks = 0;
+    glance_packed held{};             // pool == nullptr: none
     // test hook, one shot: the next glance_debug_gemm(_wide) launch withholds one ring slot and waits at most this long
     int stall_kstep1 = 0;
     unsigned long long stall_limit_ns = 0;
@@ -278,6 +290,26 @@ void attention(glance_ctx *ctx, AttnParams ap) {
     prof_end(ctx, prof, KIND_ATTN, 0.0);
 }
 
+// the same over a cache that is read in part or held in 4 bits; ap carries window and sinks
+void attention_cache(glance_ctx *ctx, AttnParams ap, int layer, int seq_off) {
+    const glance_config &c = ctx->cfg;
+    ap.trace = nullptr;
+    if (ctx->held.pool) {
+        ap.held_len = ctx->held.len + seq_off;
+        ap.held_table = ctx->held.page_table + (size_t)seq_off * c.max_pages_per_seq;
+        ap.held_pages = ctx->held.n_pages;
+        ap.held_layer = (const unsigned char *)ctx->held.pool + (size_t)layer * ctx->held.n_pages * c.n_kv_heads * packed::tile_bytes(c.head_dim);
+    }
+    ap.parts = ctx->ws.few_parts; ap.parts_ml = ctx->ws.few_ml; ap.part_counters = ctx->ws.few_counters;
+    const CUtensorMap *m = get_map(ctx, ap.pool_layer, ap.d, ap.geom.n_pages * 2 * ap.geom.n_kv_heads * kPage, kPage);
+    if (!m) return;
+    const bool few = attention_few_takes(ap.T, ap.Hq / ap.Hkv);
+    if (!few) ap.S = attention_tc_splits(ap.T, ap.Hq / ap.Hkv, ap.Hkv, ap.batch, ap.d);
+    const bool prof = prof_begin(ctx);
+    if ((few ? launch_attention_few(ap, *m, ctx->stream) : launch_attention_cache(ap, *m, ctx->stream)) != cudaSuccess) ctx->map_error = true;
+    prof_end(ctx, prof, KIND_ATTN, 0.0);
+}
+
 // row scales 1/rms from the per-tile sums of squares the producer left in ws.ssq
 void with_row_scales(const glance_ctx *ctx, TcGemmArgs &a) {
     a.ssq = ctx->ws.ssq; a.n_ssq = ctx->dims.n_ssq; a.ssq_stride = ctx->dims.Rmax; a.eps = ctx->cfg.rms_eps;
@@ -334,7 +366,8 @@ RowOut rowout_of(const glance_ctx *ctx) {
 //   O GEMM (+ residual, bf16 copy scaled by ln2, sums of squares)  ->
 //   gate/up GEMM (+ 1/rms row scale, SwiGLU)  ->  down GEMM (+ residual, bf16 copy scaled by next_gain, sums of squares)
 // On entry ws.x is the residual stream, ws.xn = bf16(x * gain) and ws.ssq its sums of squares; same on exit.
-void run_layer(glance_ctx *ctx, const LayerW &w, bf16 *pool_layer, const PassInfo &ps, const bf16 *next_gain,
+// `layer` is the target layer, or -1 in the block head (whose cache is read whole).
+void run_layer(glance_ctx *ctx, int layer, const LayerW &w, bf16 *pool_layer, const PassInfo &ps, const bf16 *next_gain,
                bf16 *hidden_out) {
     const glance_config &c = ctx->cfg;
     const Dims &d = ctx->dims;
@@ -361,14 +394,20 @@ void run_layer(glance_ctx *ctx, const LayerW &w, bf16 *pool_layer, const PassInf
         gemm(ctx, 4, wqkv, ws.xn, xr, g);
     }
     if (ps.Rq == 0) return;
-    AttnParams ap;
+    AttnParams ap{};
     ap.batch = ps.batch; ap.T = ps.T; ap.Hq = c.n_q_heads; ap.Hkv = c.n_kv_heads; ap.d = c.head_dim;
     ap.q = ws.q; ap.q_lo = ws.q + (size_t)xr * d.qd; ap.pool_layer = pool_layer; ap.geom = geom; ap.page_table = page_table; ap.seq_len = seq_len;
     ap.anc = ps.anc; ap.causal = ps.causal ? 1 : 0; ap.W = (ps.T + 63) / 64; ap.out = ws.attn; ap.out_lo = ws.attn + (size_t)xr * d.qd;
-    ap.S = attention_tc_splits(ps.T, c.n_q_heads / c.n_kv_heads, c.n_kv_heads, ps.batch, c.head_dim);
     ap.status = ws.status;
     ap.lo_skip = ctx->attn_lo_skip; ap.lo_skip_min_keys = ctx->attn_lo_min_keys;
-    attention(ctx, ap);
+    const int window = layer >= 0 && !ctx->window.empty() ? ctx->window[layer] : 0;
+    if (window > 0 || (layer >= 0 && ctx->held.pool)) {
+        ap.window = window; ap.sinks = window > 0 ? ctx->sinks : 0;
+        attention_cache(ctx, ap, layer, ps.seq_off);
+    } else {
+        ap.S = attention_tc_splits(ps.T, c.n_q_heads / c.n_kv_heads, c.n_kv_heads, ps.batch, c.head_dim);
+        attention(ctx, ap);
+    }
     const int R = ps.Rq;
     {
         TcGemmArgs g{};
@@ -405,7 +444,7 @@ void run_target(glance_ctx *ctx, const PassInfo &ps, bf16 *hidden_out, float *lo
         bf16 *tap_out = nullptr;
         for (int i = 0; i < head_depth(c) && hidden_out; ++i)
             if (head_tap(c, i) == l) tap_out = hidden_out + (size_t)i * ps.R * c.hidden;
-        run_layer(ctx, w, pool_layer, ps, last ? ctx->final_norm : ctx->ln1[l + 1], tap_out);
+        run_layer(ctx, l, w, pool_layer, ps, last ? ctx->final_norm : ctx->ln1[l + 1], tap_out);
     }
     if (argmax) {   // logits are stored only on request
         TcGemmArgs g{};
@@ -439,9 +478,10 @@ int32_t finish(glance_ctx *ctx) {
     return cudaPeekAtLastError() == cudaSuccess ? GLANCE_OK : GLANCE_E_CUDA;
 }
 
-__global__ void set_seq_kernel(int32_t *seq_len, int32_t *root, int32_t len, int32_t r) {
+__global__ void set_seq_kernel(int32_t *seq_len, int32_t *root, int32_t len, int32_t r, int32_t *held_len) {
     *seq_len = len;
     *root = r;
+    if (held_len && *held_len > len / kPage * kPage) *held_len = len / kPage * kPage;
 }
 
 }  // namespace
@@ -527,6 +567,8 @@ int32_t glance_create(const glance_config *cfg, const glance_target_weights *t, 
         cudaMemsetAsync(ws.am_keys, 0, (size_t)d.Rlog * 8, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.am_counter, 0, 256, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.wide_counters, 0, (size_t)kWideCut * 2 * 4, ctx->stream) != cudaSuccess ||
+        cudaMemsetAsync(ws.few_counters, 0, (size_t)cfg->max_batch * cfg->n_kv_heads * 4, ctx->stream) != cudaSuccess ||
+        cudaMemsetAsync(ws.pack_counter, 0, 4, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.tk_thr, 0, (size_t)cfg->max_batch * cfg->block_B * kTopkTileCap * 4, ctx->stream) != cudaSuccess) {
         delete ctx;
         return GLANCE_E_CUDA;
@@ -586,7 +628,7 @@ int32_t glance_prefill(glance_ctx *ctx, const glance_seqs *seqs, int32_t seq, co
             LayerW hw{(const bf16 *)hl.ln2, (const bf16 *)hl.wqkv, (const bf16 *)hl.wo, (const bf16 *)hl.wgu,
                       (const bf16 *)hl.wd};
             PassInfo hp{n, 0, 1, n, nullptr, true, seqs, seq};
-            run_layer(ctx, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * tg.layer_stride(), hp, nullptr, nullptr);
+            run_layer(ctx, -1, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * tg.layer_stride(), hp, nullptr, nullptr);
         }
         LAUNCH(ctx, KIND_CONTROL, launch_prefill_advance(seqs->seq_len + seq, seqs->root + seq, seqs->feat_count + seq,
                                                          last ? ws.argmax_tmp : nullptr, n, st));
@@ -599,7 +641,8 @@ int32_t glance_seq_truncate(glance_ctx *ctx, const glance_seqs *seqs, int32_t se
     if (rc) return rc;
     if (seq < 0 || seq >= seqs->batch || new_len < 0 || new_root < 0 || new_root >= ctx->cfg.vocab)
         return GLANCE_E_INVALID_ARG;
-    LAUNCH(ctx, KIND_CONTROL, (set_seq_kernel<<<1, 1, 0, ctx->stream>>>(seqs->seq_len + seq, seqs->root + seq, new_len, new_root)));
+    LAUNCH(ctx, KIND_CONTROL, (set_seq_kernel<<<1, 1, 0, ctx->stream>>>(seqs->seq_len + seq, seqs->root + seq, new_len, new_root,
+                                                               ctx->held.pool ? ctx->held.len + seq : nullptr)));
     return finish(ctx);
 }
 
@@ -633,7 +676,7 @@ int32_t glance_draft_block(glance_ctx *ctx, const glance_seqs *seqs, int32_t *to
         LayerW hw{(const bf16 *)hl.ln2, (const bf16 *)hl.wqkv, (const bf16 *)hl.wo, (const bf16 *)hl.wgu, (const bf16 *)hl.wd};
         PassInfo ps{R, R1, batch, B, nullptr, false, seqs, 0};
         const bf16 *next_gain = i + 1 < HL ? (const bf16 *)ctx->head_layer[i + 1].ln1 : (const bf16 *)ctx->head.final_norm;
-        run_layer(ctx, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * hgeom.layer_stride(), ps, next_gain, nullptr);
+        run_layer(ctx, -1, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * hgeom.layer_stride(), ps, next_gain, nullptr);
     }
     // LM head over the block rows with the per-offset top-k fused into its epilogue: every 128-feature tile leaves
     // its log-sum-exp share and the keys that can still be among a row's k largest; one small launch merges them.
@@ -743,6 +786,79 @@ int32_t glance_log_root_entropy(glance_ctx *ctx, float *entropy) {
     return GLANCE_OK;
 }
 
+int32_t glance_set_window(glance_ctx *ctx, const int32_t *window, int32_t sinks) {
+    if (!ctx || sinks < 0) return GLANCE_E_INVALID_ARG;
+    for (int l = 0; window && l < ctx->cfg.n_layers; ++l)
+        if (window[l] < 0) return GLANCE_E_INVALID_ARG;
+    try {
+        if (window) ctx->window.assign(window, window + ctx->cfg.n_layers);
+        else ctx->window.clear();
+    } catch (...) {
+        return GLANCE_E_INVALID_ARG;
+    }
+    ctx->sinks = window ? sinks : 0;
+    return GLANCE_OK;
+}
+
+size_t glance_packed_bytes(const glance_config *cfg, int32_t n_pages) {
+    if (!config_ok(cfg) || n_pages < 1) return 0;
+    return (size_t)cfg->n_layers * n_pages * cfg->n_kv_heads * packed::tile_bytes(cfg->head_dim);
+}
+
+int32_t glance_set_packed(glance_ctx *ctx, const glance_packed *packed) {
+    if (!ctx) return GLANCE_E_INVALID_ARG;
+    if (!packed) {
+        ctx->held = glance_packed{};
+        return GLANCE_OK;
+    }
+    if (packed->n_pages < 1 || !packed->len || !packed->page_table || !packed->pool || ((uintptr_t)packed->pool & 15)) return GLANCE_E_INVALID_ARG;
+    ctx->held = *packed;
+    return GLANCE_OK;
+}
+
+static int32_t pack_common(glance_ctx *ctx, const glance_seqs *seqs, int32_t keep, const int32_t *new_len) {
+    const int32_t rc = check_seqs(ctx, seqs);
+    if (rc) return rc;
+    if (keep < 0) return GLANCE_E_INVALID_ARG;
+    if (!ctx->held.pool) return GLANCE_E_STATE;
+    PackParams pp{};
+    pp.batch = seqs->batch; pp.n_layers = ctx->cfg.n_layers; pp.keep = keep; pp.seq_len = seqs->seq_len; pp.new_len = new_len;
+    pp.kv_pool = (bf16 *)seqs->kv_pool; pp.geom = geom_of(ctx, seqs); pp.page_table = seqs->page_table;
+    pp.pool4 = (unsigned char *)ctx->held.pool; pp.n_pages4 = ctx->held.n_pages; pp.page_table4 = ctx->held.page_table; pp.len = ctx->held.len;
+    pp.counter = ctx->ws.pack_counter; pp.status = ctx->ws.status;
+    LAUNCH(ctx, KIND_OTHER, launch_pack(pp, new_len != nullptr, ctx->stream));
+    return finish(ctx);
+}
+
+int32_t glance_pack_cache(glance_ctx *ctx, const glance_seqs *seqs, int32_t keep) { return pack_common(ctx, seqs, keep, nullptr); }
+
+int32_t glance_unpack_cache(glance_ctx *ctx, const glance_seqs *seqs, const int32_t *new_len) {
+    if (!new_len) return GLANCE_E_INVALID_ARG;
+    return pack_common(ctx, seqs, 0, new_len);
+}
+
+int32_t glance_attention(glance_ctx *ctx, const glance_seqs *seqs, int32_t layer, const void *q, const void *q_lo, const uint64_t *anc,
+                         int32_t T, int32_t causal, int32_t window, int32_t sinks, void *out, void *out_lo) {
+    const int32_t rc = check_seqs(ctx, seqs);
+    if (rc) return rc;
+    const glance_config &c = ctx->cfg;
+    if (!q || !out || layer < 0 || layer >= c.n_layers || T < 1 || window < 0 || sinks < 0) return GLANCE_E_INVALID_ARG;
+    if ((causal && anc) || (!causal && T > kMaxTreeN) || T > (long long)c.max_pages_per_seq * kPage ||
+        (long long)T * c.n_q_heads > 1 << 30)
+        return GLANCE_E_INVALID_ARG;
+    if (((uintptr_t)q | (uintptr_t)q_lo | (uintptr_t)out | (uintptr_t)out_lo) & 15) return GLANCE_E_INVALID_ARG;
+    AttnParams ap{};
+    ap.batch = seqs->batch; ap.T = T; ap.Hq = c.n_q_heads; ap.Hkv = c.n_kv_heads; ap.d = c.head_dim;
+    ap.q = (const bf16 *)q; ap.q_lo = (const bf16 *)q_lo; ap.geom = geom_of(ctx, seqs);
+    ap.pool_layer = (const bf16 *)seqs->kv_pool + (size_t)layer * ap.geom.layer_stride();
+    ap.page_table = seqs->page_table; ap.seq_len = seqs->seq_len; ap.anc = anc; ap.causal = causal ? 1 : 0; ap.W = (T + 63) / 64;
+    ap.out = (bf16 *)out; ap.out_lo = (bf16 *)out_lo; ap.status = ctx->ws.status;
+    ap.lo_skip = ctx->attn_lo_skip; ap.lo_skip_min_keys = ctx->attn_lo_min_keys;
+    ap.window = window; ap.sinks = window > 0 ? sinks : 0;
+    attention_cache(ctx, ap, layer, 0);
+    return finish(ctx);
+}
+
 int32_t glance_poll_status(glance_ctx *ctx, int32_t *device_status) {
     if (!ctx || !device_status) return GLANCE_E_INVALID_ARG;
     int32_t v = 0;
@@ -761,7 +877,7 @@ int32_t glance_debug_attention(glance_ctx *ctx, const glance_seqs *seqs, int32_t
     if (!q || !out || layer < 0 || layer >= c.n_layers || T < 1 || T > std::max(c.tree_N, c.block_B))
         return GLANCE_E_INVALID_ARG;
     const KvGeom geom = geom_of(ctx, seqs);
-    AttnParams ap;
+    AttnParams ap{};
     ap.batch = seqs->batch; ap.T = T; ap.Hq = c.n_q_heads; ap.Hkv = c.n_kv_heads; ap.d = c.head_dim;
     ap.q = (const bf16 *)q; ap.q_lo = (const bf16 *)q_lo; ap.pool_layer = (const bf16 *)seqs->kv_pool + (size_t)layer * geom.layer_stride();
     ap.geom = geom; ap.page_table = seqs->page_table; ap.seq_len = seqs->seq_len; ap.anc = anc; ap.causal = 0; ap.W = (T + 63) / 64;

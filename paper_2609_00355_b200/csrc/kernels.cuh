@@ -103,6 +103,23 @@ void launch_walk_commit(const WalkCommit &p, cudaStream_t st);
 void launch_prefill_advance(int32_t *seq_len, int32_t *root, int32_t *feat_count, const int32_t *argmax, int count,
                             cudaStream_t st);
 
+// ---- 4-bit cache (pack_cache.cu) ----------------------------------------------------------
+struct PackParams {
+    int batch, n_layers, keep;
+    const int32_t *seq_len;
+    const int32_t *new_len;      // way back: [batch]
+    bf16 *kv_pool;
+    KvGeom geom;
+    const int32_t *page_table;
+    unsigned char *pool4;        // (layer, page, kv head) tiles of packed.cuh
+    int n_pages4;
+    const int32_t *page_table4;
+    int32_t *len;                // [batch] positions held in 4 bits
+    int32_t *counter;            // zero between launches
+    int32_t *status;
+};
+void launch_pack(const PackParams &p, bool back, cudaStream_t st);
+
 // ---- attention (attention_tc.cu) ----------------------------------------------------------
 struct AttnParams {
     int batch, T, Hq, Hkv, d;    // T = query rows per sequence = extra (uncommitted) keys per sequence
@@ -125,9 +142,24 @@ struct AttnParams {
     int lo_skip, lo_skip_min_keys;
     int32_t *status;
     unsigned long long *trace;   // test hook: phase timestamps of the first CTA, or nullptr
+    // a cache that is not read whole (attention_few.cu, the CACHE variants of attention_tc.cu)
+    int window, sinks;           // row at position a sees p < sinks and p > a - window; window 0: no limit
+    const int32_t *held_len;     // [batch] positions held in 4 bits, or nullptr: none
+    const unsigned char *held_layer;   // (page, kv head) tiles of packed.cuh
+    const int32_t *held_table;   // [batch][max_pages_per_seq]
+    int held_pages;
+    float *parts, *parts_ml;     // workspace: [2 * CTAs][kFewRows][d], [..][kFewRows][2]
+    int32_t *part_counters;      // [batch * Hkv], zero between launches
 };
+// few query rows over a cache read in part: at most kFewRows packed rows (T * heads of a kv head)
+constexpr int kFewRows = 32;
+constexpr int kFewParts = 2 * 2 * 148;       // partial results of a launch: two a CTA, two CTAs an SM
+bool attention_few_takes(int T, int G);
+cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 // map_kv = 2-D map of the pool layer {d, n_pages*2*Hkv*64 rows}, box {64, 64}
 cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
+// the same for a cache that is read in part or held in 4 bits (window, sinks, held_*)
+cudaError_t launch_attention_cache(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 CtaSize attention_tc_cta_size(int d);
 int attention_tc_q_tiles(int T, int G);
 int attention_tc_splits(int T, int G, int Hkv, int batch, int d);

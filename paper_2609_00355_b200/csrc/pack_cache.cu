@@ -1,0 +1,193 @@
+// Moves finished pages of the target's cache into the 4-bit pool and back (format: packed.cuh).
+//
+// HBM-bound: 2 bytes of a value are read and 9/16 of one written, or the other way round.  One wave of blocks takes the tiles
+// (layer, page, kv head, K|V) in turn; which pages are due is worked out from the device-resident lengths by every block.  A
+// lane takes one group of 16 values: two 16-byte loads, the scale, eight conversions, one 8-byte store; the loads of a
+// thread's next group are in flight while it converts.  The block that is the last to have read the lengths publishes the new
+// ones (nothing else in the launch reads what it writes), so nobody waits for the copies.
+#include <cuda_fp8.h>
+
+#include "kernels.cuh"
+#include "packed.cuh"
+
+namespace glance {
+
+namespace {
+
+using namespace packed;
+
+constexpr int kPackThreads = 256;
+constexpr int kMaxSeqs = 64;
+
+__device__ __forceinline__ int whole_pages(int n) { return max(n, 0) / kPage; }
+
+// e4m3 of a / 6 for a = max|x| >= 0: both roundings (the quotient's to fp32, its to e4m3) act as one, because a has eight
+// significant bits: a / 6 is either a border of e4m3 exactly or further from one than fp32 rounds.
+__device__ __forceinline__ uint32_t scale_code(float a) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 x;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %1, %2;\n\tcvt.u32.u16 %0, x;\n\t}" : "=r"(r) : "f"(0.f), "f"(__fdiv_rn(a, 6.f)));
+    return r & 0xffu;
+}
+// e2m1 of x / s for two values (a in the low nibble), r = 1 / s rounded.  A quotient of an eight-bit and a four-bit
+// significand is a border of e2m1 (an odd multiple of 1/4, 1/2 or 1) exactly or at least 2^-10 away from one.  So it may be
+// rounded to a multiple of 2^-13, which undoes the rounding of r (2^-20 at most where it matters) and keeps ties ties.
+__device__ __forceinline__ uint32_t value_codes(float a, float b, float r) {
+    constexpr float kGrid = 1536.f;                      // 1.5 * 2^10: its last place is 2^-13
+    const float qa = __fsub_rn(__fmaf_rn(a, r, kGrid), kGrid), qb = __fsub_rn(__fmaf_rn(b, r, kGrid), kGrid);
+    uint32_t c;
+    asm("{\n\t.reg .b8 x;\n\t.reg .b16 y;\n\tcvt.rn.satfinite.e2m1x2.f32 x, %1, %2;\n\tmov.b16 y, {x, 0};\n\tcvt.u32.u16 %0, y;\n\t}" : "=r"(c) : "f"(qb), "f"(qa));
+    return c & 0xffu;
+}
+
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// 16 bf16 values -> 8 bytes of codes and the scale's code
+__device__ __forceinline__ uint2 pack_group(const uint4 (&v)[2], uint32_t &scale) {
+    const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    uint32_t top = 0;                                    // the largest magnitude, by its bits
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+    scale = top >= 0x7f80u ? 0x7fu : scale_code(__uint_as_float(top << 16));
+    __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)scale, __NV_E4M3);
+    const float s = __half2float(__half(h));
+    const bool live = s > 0.f;                           // a scale of 0 or NaN: codes 0
+    const float r = __frcp_rn(s);
+    uint2 out = make_uint2(0u, 0u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t c = live ? value_codes(bf_lo(w[i]), bf_hi(w[i]), r) : 0u;
+        (i < 4 ? out.x : out.y) |= c << (8 * (i & 3));
+    }
+    return out;
+}
+
+__device__ __forceinline__ void unpack_group(uint2 c, uint32_t scale, uint4 (&v)[2]) {
+    const uint32_t s = scales_to_half(scale | scale << 8);
+    uint32_t h[4], r[8];
+    codes_to_half(c.x, h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = half2_to_bf16(mul_half2(h[i], s));
+    codes_to_half(c.y, h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[4 + i] = half2_to_bf16(mul_half2(h[i], s));
+    v[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    v[1] = make_uint4(r[4], r[5], r[6], r[7]);
+}
+
+template <int D, bool BACK>
+__global__ void __launch_bounds__(kPackThreads) pack_kernel(PackParams p) {
+    constexpr int GROUPS = Tile<D>::GROUPS;
+    __shared__ int sh_first[kMaxSeqs], sh_upto[kMaxSeqs + 1], sh_len[kMaxSeqs];      // first page due, pages due up to here, new length
+    __shared__ int sh_last;
+    const int t = threadIdx.x;
+    if (t < p.batch) {
+        const int cap = p.geom.max_pages_per_seq;
+        const int seen = max(p.seq_len[t], 0);
+        const int have = min(min(whole_pages(p.len[t]), whole_pages(seen)), cap);      // a length beyond seq_len counts for nothing
+        int lo, hi;
+        if (BACK) {
+            lo = min(whole_pages(p.new_len[t]), have);
+            hi = have;
+            sh_len[t] = lo * kPage;
+        } else {
+            lo = have;
+            hi = max(min(whole_pages(seen - p.keep), cap), have);
+            sh_len[t] = hi * kPage;
+            if (whole_pages(seen) > cap) set_status(p.status, GLANCE_E_CAPACITY);
+        }
+        sh_first[t] = lo;
+        sh_upto[t + 1] = hi - lo;
+    }
+    __syncthreads();
+    if (t == 0) {
+        sh_upto[0] = 0;
+        for (int s = 0; s < p.batch; ++s) sh_upto[s + 1] += sh_upto[s];
+        // counted in once the lengths are read (they were, by threads before the barrier)
+        __threadfence();
+        sh_last = atomicAdd(p.counter, 1) == (int)gridDim.x - 1;
+        if (sh_last) *p.counter = 0;
+    }
+    __syncthreads();
+    if (sh_last && t < p.batch) p.len[t] = sh_len[t];
+
+    const int pages = sh_upto[p.batch];
+    const int H = p.geom.n_kv_heads;
+    const size_t layer4 = (size_t)p.n_pages4 * H * Tile<D>::BYTES;
+    // item: layer, page, head, K|V
+    const long long items = (long long)pages * p.n_layers * H * 2;
+    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+        const int kvh = (int)(it % (2 * H));
+        const long long rest = it / (2 * H);
+        const int pg = (int)(rest % pages), layer = (int)(rest / pages);
+        const int kv = kvh & 1, head = kvh >> 1;
+        int s = 0;
+        while (sh_upto[s + 1] <= pg) ++s;
+        const int page = sh_first[s] + pg - sh_upto[s];
+        const int from = p.page_table[(size_t)s * p.geom.max_pages_per_seq + page];
+        const int at4 = p.page_table4[(size_t)s * p.geom.max_pages_per_seq + page];
+        if (from < 0 || from >= p.geom.n_pages || at4 < 0 || at4 >= p.n_pages4) {
+            if (t == 0) set_status(p.status, GLANCE_E_BOUNDS);
+            continue;
+        }
+        bf16 *rows = p.kv_pool + (size_t)layer * p.geom.layer_stride() + p.geom.row(from, kv, head, 0);
+        unsigned char *tile = p.pool4 + layer * layer4 + ((size_t)at4 * H + head) * Tile<D>::BYTES + kv * Tile<D>::HALF;
+        constexpr int STEPS = kPage * GROUPS / kPackThreads;
+        static_assert(kPage * GROUPS % kPackThreads == 0, "whole steps");
+        if (!BACK) {
+            uint4 v[STEPS][2];
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(rows) + (size_t)(u * kPackThreads + t) * 2;
+                v[u][0] = __ldcs(src);
+                v[u][1] = __ldcs(src + 1);
+            }
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int g = u * kPackThreads + t, key = g / GROUPS, c = g % GROUPS;
+                uint32_t scale;
+                const uint2 codes = pack_group(v[u], scale);
+                *reinterpret_cast<uint2 *>(tile + code_at<D>(key, c >> 1) + (c & 1) * 8) = codes;
+                // four neighbours' scales in one store
+                uint32_t four = scale << (8 * (t & 3));
+                four |= __shfl_xor_sync(0xffffffffu, four, 1);
+                four |= __shfl_xor_sync(0xffffffffu, four, 2);
+                if ((t & 3) == 0) *reinterpret_cast<uint32_t *>(tile + Tile<D>::SCALES + g) = four;
+            }
+        } else {
+            uint2 codes[STEPS];
+            uint32_t scale[STEPS];
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int g = u * kPackThreads + t, key = g / GROUPS, c = g % GROUPS;
+                codes[u] = __ldcs(reinterpret_cast<const uint2 *>(tile + code_at<D>(key, c >> 1) + (c & 1) * 8));
+                scale[u] = tile[Tile<D>::SCALES + g];
+            }
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                uint4 v[2];
+                unpack_group(codes[u], scale[u], v);
+                uint4 *dst = reinterpret_cast<uint4 *>(rows) + (size_t)(u * kPackThreads + t) * 2;
+                dst[0] = v[0];
+                dst[1] = v[1];
+            }
+        }
+    }
+}
+
+}  // namespace
+
+void launch_pack(const PackParams &p, bool back, cudaStream_t st) {
+    // one wave: every block has to be counted in before the lengths may change, and a block strides over the tiles
+    const long long most = (long long)p.batch * p.geom.max_pages_per_seq * p.n_layers * p.geom.n_kv_heads * 2;
+    const int blocks = (int)(most < 148 * 8 ? most : 148 * 8);
+    if (p.geom.head_dim == 128) {
+        if (back) pack_kernel<128, true><<<blocks, kPackThreads, 0, st>>>(p);
+        else pack_kernel<128, false><<<blocks, kPackThreads, 0, st>>>(p);
+    } else {
+        if (back) pack_kernel<64, true><<<blocks, kPackThreads, 0, st>>>(p);
+        else pack_kernel<64, false><<<blocks, kPackThreads, 0, st>>>(p);
+    }
+}
+
+}  // namespace glance

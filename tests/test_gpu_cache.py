@@ -1,0 +1,313 @@
+"""Attention over a cache that is read in part (sliding window, sinks) or held in 4 bits, and the packing of that cache (GPU).
+
+References are written from the definitions in 64 bits.  Tolerances, derived before the first run, with A = sum_j p_j |v_j|
+(what the output would be without cancellation):
+  * out is bf16: half a step, 2^-8 of the value;
+  * probabilities are rounded to fp16 or to two terms: 2^-11 of A at most;
+  * scores are fp32 sums of d products: (d + 2) 2^-24 sum |q||k| / sqrt(d), below 2 x 10^-4 for the inputs here (sum |q||k| /
+    sqrt(d) < 13 on average over a row); numerator and denominator each carry it: less than 2^-11 of A together;
+so |out - ref| <= 2^-8 |ref| + 2^-10 A.  With two-term queries and outputs (hi + lo: 2^-16) and two-term probabilities
+(2^-16) only the scores' error stays: 2^-15 |ref| + 2^-11 A.
+"""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_00355_b200 import synth
+
+PAGE, GROUP = 64, 16
+
+
+# ---- definitions in 64 bits ----------------------------------------------------------------------------------------
+def held_values(x):
+    """What groups of 16 along the last axis are held as: e2m1 codes with an e4m3 scale, ties to the even code."""
+    g = x.double().unflatten(-1, (-1, GROUP))
+    a = g.abs().amax(-1, keepdim=True) / 6
+    step = torch.exp2(torch.floor(torch.log2(a.clamp(min=2.0 ** -40))).clamp(min=-6) - 3)
+    s = (torch.round(a / step) * step).clamp(max=448)
+    m = torch.where(s > 0, g.abs() / torch.where(s > 0, s, 1.0), 0.0)
+    unit = torch.where(m < 2, 0.5, torch.where(m < 4, 1.0, 2.0)).double()
+    v = torch.copysign((torch.round(m / unit) * unit).clamp(max=6), g) * s
+    v = torch.where(torch.isfinite(g).all(-1, keepdim=True), v, math.nan)
+    return v.flatten(-2)
+
+
+def visible(P, T, kind, parents, window, sinks):
+    """[T][P + T] truth values: which cache rows each row sees."""
+    see = np.ones((T, P + T), dtype=bool)
+    at = np.arange(P + T)
+    if kind == "tree":
+        see[:, P:] = False
+        for i in range(T):
+            j, chain = i, []
+            while j >= 0:
+                see[i, P + j] = True
+                chain.append(j)
+                j = int(parents[j])
+            at[P + i] = P + len(chain) - 1
+    elif kind == "chain":
+        see[:, P:] = np.tri(T, dtype=bool)
+    if window:
+        for i in range(T):
+            see[i] &= (at < sinks) | (at[P + i] - at < window)
+    return see
+
+
+def reference(q, K, V, see):
+    """q [T][Hq][d], K, V [P + T][Hkv][d] float64 -> out [T][Hq][d] and A.  Rows that see nothing are zeros."""
+    T, Hq, d = q.shape
+    G = Hq // K.shape[1]
+    see = torch.from_numpy(see).to(q.device)
+    out, A = torch.zeros_like(q), torch.zeros_like(q)
+    some = see.any(1)
+    used = see.any(0)
+    for h in range(Hq):
+        k, v = K[used, h // G], V[used, h // G]
+        s = (q[:, h] @ k.T / math.sqrt(d)).masked_fill(~see[:, used], -math.inf)
+        p = torch.softmax(s[some], dim=1)
+        out[some, h] = p @ v
+        A[some, h] = p @ v.abs()
+    return out, A
+
+
+def random_parents(T, rng):
+    parents = np.full(T, -1)
+    nodes = T - (int(rng.integers(0, T // 8 + 1)) if T > 8 else 0)
+    for i in range(1, nodes):
+        parents[i] = i - 1 if rng.random() < 0.6 else int(rng.integers(max(0, i - 12), i))
+    return parents
+
+
+def anc_words(parents):
+    T = len(parents)
+    W = (T + 63) // 64
+    words = np.zeros((T, W), dtype=np.uint64)
+    for i in range(T):
+        j = i
+        while j >= 0:
+            words[i, j // 64] |= np.uint64(1) << np.uint64(j % 64)
+            j = int(parents[j])
+    return words.view(np.int64)
+
+
+# ---- engine whose cache is ours --------------------------------------------------------------------------------------
+def make_engine(heads, batch, max_len, layers=1, stream=None):
+    from paper_2609_00355_b200.binding import Engine
+    Hq, Hkv, d = heads
+    cfg = synth.RoundConfig(name="cache", n_layers=layers, hidden=64, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, ffn=64, vocab=64, n_img=0,
+                            n_txt=0, block_B=16, topk=1, tree_N=128, p_m=0.8, rounds=1, batch=batch)
+    tw, hw = synth.make_weights(cfg, "cuda")
+    eng = Engine(cfg, tw, hw, batch=batch, max_len=max_len, stream=stream)
+    return eng
+
+
+class Cache:
+    """An engine, random cache contents, and what they are in 64 bits."""
+
+    def __init__(self, heads, lens, T, seed, held=None, layers=1, junk=True, stream=None):
+        from paper_2609_00355_b200.binding import PackedCache
+        self.heads, self.lens, self.T = heads, lens, T
+        Hq, Hkv, d = heads
+        batch = len(lens)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.eng = eng = make_engine(heads, batch, max(lens) + T, layers, stream)
+        loud = torch.exp(0.5 * torch.randn(Hkv, 1, d, device="cuda", generator=g))
+        pool = torch.randn(eng.kv_pool.shape, device="cuda", generator=g)
+        pool[:, :, 0] *= loud
+        eng.kv_pool.copy_(pool)
+        eng.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        self.K, self.V = [], []
+        for s, P in enumerate(lens):
+            K, V = eng.gather_kv(s, 0, P + T)
+            self.K.append(K.double())
+            self.V.append(V.double())
+        if junk:                                          # places beyond the last row hold anything
+            for s, P in enumerate(lens):
+                at = (P + T) % PAGE
+                if at:
+                    eng.kv_pool[:, int(eng.page_table[s, (P + T) // PAGE]), :, :, at:] = math.nan
+        if held is not None:
+            self.packed = PackedCache(eng)
+            # (pages in an order of their own)
+            self.packed.page_table.copy_(torch.randperm(batch * eng.pages_per_seq, generator=torch.Generator().manual_seed(seed)).to(torch.int32).view(batch, -1))
+            eng.glance_set_packed(self.packed)
+            eng.glance_pack_cache(keep=held)
+            assert self.packed.len.tolist() == [max(0, P - held) // PAGE * PAGE for P in lens]
+            for s, n in enumerate(self.packed.len.tolist()):
+                self.K[s][:n] = held_values(self.K[s][:n])
+                self.V[s][:n] = held_values(self.V[s][:n])
+                for p in range(n // PAGE):                # the bf16 pages are not read any more
+                    eng.kv_pool[:, int(eng.page_table[s, p])] = math.nan
+            eng.page_table.copy_(torch.where(torch.arange(eng.pages_per_seq, device="cuda")[None] < self.packed.len[:, None] // PAGE, -7, eng.page_table))
+        self.q = torch.randn(batch * T, Hq * d, device="cuda", generator=g).to(torch.bfloat16)
+
+    def hide(self, see):
+        """NaN at cache rows that no row sees (before packing keeps them out of the 4-bit part's groups: whole rows)."""
+        for s, P in enumerate(self.lens):
+            dead = torch.from_numpy(~see[s].any(0)).nonzero().flatten().tolist()
+            for p in dead:
+                page = int(self.eng.page_table[s, p // PAGE])
+                if page >= 0:
+                    self.eng.kv_pool[:, page, :, :, p % PAGE] = math.nan
+
+
+def check(out, ref, A, two=False):
+    tol = (2.0 ** -15 * ref.abs() + 2.0 ** -11 * A) if two else (2.0 ** -8 * ref.abs() + 2.0 ** -10 * A)
+    err = (out.double() - ref).abs()
+    assert bool(torch.isfinite(out.double()).all())
+    assert bool((err <= tol + 1e-30).all()), float((err / (tol + 1e-30)).max())
+
+
+def run_attention(cache, kind, window, sinks, seed, two=False, hide=True):
+    eng, T = cache.eng, cache.T
+    Hq, Hkv, d = cache.heads
+    rng = np.random.default_rng(seed)
+    batch = len(cache.lens)
+    parents = [random_parents(T, rng) for _ in range(batch)] if kind == "tree" else [None] * batch
+    see = [visible(P, T, kind, parents[s], window, sinks) for s, P in enumerate(cache.lens)]
+    if hide:
+        cache.hide(see)
+    anc = torch.from_numpy(np.stack([anc_words(p) for p in parents])).cuda() if kind == "tree" else None
+    q = cache.q
+    q_lo = ((torch.randn(q.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)) * 2.0 ** -9) * q.float().abs()).to(torch.bfloat16) if two else None
+    n = batch * T
+    guard = torch.full((n + 2, Hq * d), 7.0, dtype=torch.bfloat16, device="cuda")      # rows around the output stay as they are
+    out = guard[1 : n + 1]
+    lo = torch.zeros_like(q) if two else None
+    eng.glance_attention(0, q, T, out, anc=anc, causal=kind == "chain", window=window, sinks=sinks, q_lo=q_lo, out_lo=lo)
+    eng.check_device_status()
+    assert bool((guard[0] == 7).all()) and bool((guard[-1] == 7).all())
+    qd = q.double() + (q_lo.double() if two else 0)
+    for s in range(batch):
+        ref, A = reference(qd[s * T : (s + 1) * T].view(T, Hq, d), cache.K[s], cache.V[s], see[s])
+        got = out[s * T : (s + 1) * T].view(T, Hq, d).double()
+        if two:
+            got = got + lo[s * T : (s + 1) * T].view(T, Hq, d).double()
+        check(got, ref, A, two)
+    again = torch.empty_like(out)
+    eng.glance_attention(0, q, T, again, anc=anc, causal=kind == "chain", window=window, sinks=sinks, q_lo=q_lo)
+    eng.check_device_status()
+    if not two:
+        assert torch.equal(again, out)                   # the same bits, whatever the timing
+    return out
+
+
+H7, HS, HT = (28, 4, 128), (16, 4, 64), (4, 2, 64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS, HT, (8, 8, 128), (32, 8, 128), (16, 1, 64), (6, 2, 64)])
+@pytest.mark.parametrize("layers,lens,tail", [(1, [64], 0), (2, [700, 63, 128, 1000], 0), (3, [130, 500], 65), (1, [0, 1, 64 * 9], 1)])
+def test_pack_and_unpack(heads, layers, lens, tail):
+    from paper_2609_00355_b200.binding import PackedCache
+    eng = make_engine(heads, len(lens), max(lens) + 1, layers)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    # magnitudes over the format's whole range and beyond: scales that round to 0, subnormal ones, saturated ones
+    mag = torch.exp2(torch.randint(-14, 13, eng.kv_pool.shape[:-1] + (eng.kv_pool.shape[-1] // GROUP,), device="cuda", generator=g).float())
+    x = (torch.randn(eng.kv_pool.shape, device="cuda", generator=g).unflatten(-1, (-1, GROUP)) * mag[..., None]).flatten(-2).to(torch.bfloat16)
+    # ties of the scale and of the codes are common among values of three bits
+    x[:, :, :, :, ::2] = (torch.randint(-15, 16, x[:, :, :, :, ::2].shape, device="cuda", generator=g) * 0.25).to(torch.bfloat16)
+    eng.kv_pool.copy_(x)
+    eng.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+    packed = PackedCache(eng)
+    eng.glance_set_packed(packed)
+    eng.glance_pack_cache(keep=tail)
+    eng.check_device_status()
+    want = [max(0, P - tail) // PAGE * PAGE for P in lens]
+    assert packed.len.tolist() == want
+    assert torch.equal(eng.kv_pool, x)                   # the bf16 pages are left as they are
+    # a part of it back: only pages from there on
+    back = torch.full_like(x, 3.0)
+    cut = [n // 2 for n in want]
+    eng.glance_unpack_cache(torch.tensor(cut, dtype=torch.int32, device="cuda"), kv_pool=back)
+    eng.check_device_status()
+    assert packed.len.tolist() == [c // PAGE * PAGE for c in cut]
+    def pages(a, b):
+        return [int(eng.page_table[s, p]) for s in range(len(lens)) for p in range(a[s] // PAGE, b[s] // PAGE)]
+    low = [c // PAGE * PAGE for c in cut]
+    ref = torch.full(x.shape, 3.0, dtype=torch.float64, device="cuda")
+    for p in pages(low, want):
+        ref[:, p] = held_values(x[:, p])
+    assert torch.equal(back.double(), ref)
+    # the rest, and a length beyond what is held changes nothing
+    eng.glance_unpack_cache(torch.full((len(lens),), 1 << 30, dtype=torch.int32, device="cuda"), kv_pool=back)
+    assert torch.equal(back.double(), ref)
+    eng.glance_unpack_cache(torch.zeros(len(lens), dtype=torch.int32, device="cuda"))
+    eng.check_device_status()
+    assert packed.len.tolist() == [0] * len(lens)
+    ref = x.double()
+    for p in pages([0] * len(lens), low):
+        ref[:, p] = held_values(x[:, p])
+    assert torch.equal(eng.kv_pool.double(), ref)
+
+
+@pytest.mark.gpu
+def test_pack_groups_that_are_not_finite_and_signs():
+    from paper_2609_00355_b200.binding import PackedCache
+    eng = make_engine((4, 2, 64), 1, 128)
+    x = torch.randn(eng.kv_pool.shape, device="cuda").to(torch.bfloat16)
+    x[..., 3, 5] = math.inf
+    x[..., 4, 17] = -math.inf
+    x[..., 5, 63] = math.nan
+    x[..., 6, :16] = 0.0
+    x[..., 7, :16] = 3e38
+    x[..., 8, :16] = 1e-38
+    eng.kv_pool.copy_(x)
+    eng.seq_len.fill_(64)
+    eng.glance_set_packed(PackedCache(eng))
+    eng.glance_pack_cache()
+    eng.glance_unpack_cache(torch.zeros(1, dtype=torch.int32, device="cuda"))
+    eng.check_device_status()
+    page = int(eng.page_table[0, 0])
+    got, ref = eng.kv_pool[:, page].double(), held_values(x[:, page])
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)) and torch.equal(torch.nan_to_num(got), torch.nan_to_num(ref))
+
+
+CASES = [
+    # kind, T, lens, window, sinks
+    ("block", 1, [1536], 512, 4), ("block", 1, [0], 1, 0), ("block", 1, [0, 1, 63, 64, 65], 64, 1), ("block", 1, [700, 5, 2000], 1, 0),
+    ("block", 1, [2100], 2000, 1), ("block", 1, [3000, 1500], 63, 64), ("block", 1, [900], 65, 129), ("block", 1, [500], 5000, 7),
+    ("block", 1, [500], 100, 4000), ("block", 1, [40], 20, 10), ("block", 2, [640], 64, 0), ("block", 4, [333, 1], 130, 3), ("block", 16, [1000], 7, 2),
+    ("tree", 2, [128], 1, 0), ("tree", 5, [777, 64], 3, 1), ("tree", 8, [1000], 300, 66), ("tree", 17, [450, 20], 4, 30),
+    ("tree", 64, [1536], 700, 4), ("tree", 65, [100, 3000], 64, 64), ("tree", 128, [2048], 1000, 100), ("tree", 128, [5], 6, 8), ("tree", 33, [0], 2, 1),
+    ("chain", 3, [70], 2, 1), ("chain", 129, [0], 40, 3), ("chain", 500, [333], 100, 5), ("chain", 300, [64], 1, 0), ("chain", 200, [1000], 1000, 1100),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS, (8, 8, 128), (16, 1, 64)])
+@pytest.mark.parametrize("kind,T,lens,window,sinks", CASES)
+def test_window(heads, kind, T, lens, window, sinks):
+    run_attention(Cache(heads, lens, T, 11), kind, window, sinks, 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS, (8, 8, 128), (16, 1, 64)])
+@pytest.mark.parametrize("kind,T,lens,held", [
+    ("block", 1, [64], 0), ("block", 1, [1536], 0), ("block", 1, [5000, 300, 64, 0], 64), ("block", 2, [900], 1), ("block", 16, [400, 1500], 130),
+    ("tree", 7, [1000], 0), ("tree", 20, [129, 4000], 64), ("tree", 64, [1536], 64), ("tree", 128, [700, 64], 0), ("tree", 100, [20], 0),
+    ("chain", 2, [191], 0), ("chain", 400, [512], 0), ("chain", 130, [3000], 500)])
+def test_packed(heads, kind, T, lens, held):
+    run_attention(Cache(heads, lens, T, 12, held=held), kind, 0, 0, 4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS, HT])
+@pytest.mark.parametrize("held", [0, 100, 400])
+@pytest.mark.parametrize("kind,T,lens,window,sinks", [
+    ("block", 1, [1536, 700], 512, 4), ("block", 1, [1000], 70, 130), ("block", 3, [1000, 100], 200, 64), ("tree", 9, [900], 150, 70),
+    ("tree", 64, [1536], 300, 4), ("tree", 80, [2000, 500], 450, 200), ("chain", 300, [900], 333, 65), ("chain", 10, [500], 60, 1)])
+def test_packed_window(heads, held, kind, T, lens, window, sinks):
+    run_attention(Cache(heads, lens, T, 13, held=held), kind, window, sinks, 5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS])
+@pytest.mark.parametrize("held", [None, 64])
+@pytest.mark.parametrize("kind,T,lens,window,sinks", [("block", 1, [1536], 512, 4), ("tree", 4, [1000, 300], 300, 4), ("tree", 64, [1536], 700, 4),
+                                                      ("chain", 200, [700], 300, 64)])
+def test_two_terms(heads, held, kind, T, lens, window, sinks):
+    run_attention(Cache(heads, lens, T, 14, held=held), kind, window, sinks, 6, two=True)
