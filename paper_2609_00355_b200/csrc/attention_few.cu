@@ -2,10 +2,10 @@
 // window, sinks) or held in 4 bits: bound by the bytes of the cache, so everything is laid out around streaming them once.
 //
 // The pages that a launch has to read form one line: sequences, in each its kv heads, in each the pages that some row sees
-// (packed.cuh).  The line is dealt out in equal stretches to two CTAs an SM, so ragged batches and long single sequences
-// keep the whole GPU reading; a CTA finds its stretch from the device-resident lengths by one prefix sum.  Warp 4 fetches
-// pages into a ring (bf16: two tensor copies; 4 bits: one bulk copy of a 4.5-bit tile, three of which fit where a bf16 page
-// does), warps 0..3 take 16 of a page's 64 keys each and never wait for one another inside an item.
+// (packed.cuh).  The line is dealt out in equal stretches to one CTA an SM, so ragged batches and long single sequences
+// keep the whole GPU reading; a CTA finds its stretch from the device-resident lengths by one prefix sum.  Teams of four warps
+// take its pages in turn, a warp 16 of a page's 64 keys, and nobody waits for another inside an item; a team's producer warp
+// fetches its pages into its ring (bf16: tensor copies; 4 bits: one bulk copy of a 4.5-bit tile).
 //     S^T[16 keys x 8 rows] = K Q^T,   O^T[d x 8 rows] += V^T P^T     (mma.sync m16n8k16, fp32 accumulators)
 // Keys sit in the M dimension, so one token's 7 or 8 heads fill an instruction's N exactly; with rows in M half of it
 // would idle, and 128-row tcgen05 tiles would run at 6 % and wait for their tensor memory round trips.  At 8 rows a page
@@ -18,6 +18,7 @@
 // The warps' partial results meet in shared memory; an item that several CTAs share is finished by the one that comes last,
 // which adds the parts in line order, so results do not depend on timing.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.cuh"
 #include "packed.cuh"
@@ -30,25 +31,34 @@ namespace {
 using namespace tc;
 using namespace packed;
 
-constexpr int kWarps = 4;                    // consumer warps
-constexpr int kFewThreads = (kWarps + 1) * 32;
+constexpr int kTeam = 4;                     // consumer warps that share a page, 16 keys each
 constexpr int kMaxSeqs = 64;
 constexpr float kRaise = 8.f;                // log2 units a score may exceed its reference by
+constexpr int kEven = 6;
 
+// NB: blocks of 8 query rows.  As many teams as the registers of NB blocks' accumulators leave room for: a page's chain
+// (codes, first products, softmax, second products) is long, and only other warps' pages hide it.
 template <int D, int NB>
 struct Few {
-    static constexpr int SUB = D == 128 ? 11264 : 6144;      // one 4-bit tile (multiple of 1024: three make room for a bf16 page)
-    static constexpr int SLOTS = NB == 4 ? 15 : 6;
-    static constexpr int RING = SLOTS * SUB;
-    static constexpr int PAGE_BYTES = 2 * kPage * D * 2;     // K and V of a bf16 page
+    static constexpr int TEAMS = NB == 1 ? 3 : NB == 2 ? 2 : 1;
+    static constexpr int WARPS = TEAMS * kTeam;              // consumers; one more fetches
+    static constexpr int THREADS = (WARPS + TEAMS) * 32;
+    // A team has a ring of its own, filled by a warp of its own (a thread that waits, announces and copies takes 270 ns a
+    // page, more than a 4-bit page's share of HBM).  The ring: places of a bf16 page (K and V, multiples of 1024 for the
+    // swizzle), each of which takes three 4-bit tiles in its thirds; a bf16 page goes to a whole place.
+    static constexpr int PAGE_BYTES = 2 * kPage * D * 2;
+    static constexpr int THIRD = PAGE_BYTES / 3 / 16 * 16;
+    static constexpr int PLACES = NB == 4 ? 4 : 2;           // a team
+    static constexpr int SLOTS = 3 * PLACES;
+    static constexpr int RING = TEAMS * PLACES * PAGE_BYTES;
     static constexpr int ROWF = D + 4;
     static constexpr int QB = 8 * D * 2;                     // one term of 8 rows' queries
     static constexpr int Q_AT = RING;                        // [fp16 | bf16][term][NB] fragments
-    static constexpr int RED_AT = Q_AT + 4 * NB * QB;        // [warp][8][ROWF] partial outputs of 8 rows
-    static constexpr int TOTAL = RED_AT + kWarps * 8 * ROWF * 4 + 1024;
-    static constexpr int CTAS = NB == 4 ? 1 : 2;             // an SM
-    static_assert(3 * SUB >= PAGE_BYTES && SUB >= Tile<D>::BYTES && SLOTS % 3 == 0, "ring");
-    static_assert(CTAS * (TOTAL + 4096) <= 228 * 1024, "CTAs an SM");
+    static constexpr int RED_AT = Q_AT + 4 * NB * QB;        // [warp of a team][8][ROWF] partial outputs of 8 rows
+    static constexpr int TOTAL = RED_AT + kTeam * 8 * ROWF * 4 + 1024;
+    static_assert(PAGE_BYTES % 1024 == 0 && THIRD >= Tile<D>::BYTES, "ring");
+    static_assert(TEAMS * NB <= kTeam, "the teams' sums of an item fit the partial outputs' place");
+    static_assert(TOTAL + 3072 <= 227 * 1024, "one CTA an SM");
 };
 
 // key of row r of a 16-key tile (r < 8; the other eight follow 8 later): eight keys that lanes read side by side differ in
@@ -58,11 +68,21 @@ __device__ __forceinline__ int key_of(int r) { return (r & 1) ? 4 + ((r >> 1) ^ 
 template <bool HALF>
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (HALF)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the same without an accumulator to add to
+template <bool HALF>
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (HALF)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&a)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]) : "r"(addr) : "memory");
@@ -97,9 +117,9 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
                  ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 
-template <int SLOTS>
+template <int TEAMS, int SLOTS>
 struct alignas(8) FewBars {
-    uint64_t full[SLOTS], empty[SLOTS];
+    uint64_t full[TEAMS][SLOTS], empty[TEAMS][SLOTS];
     int abort_flag, last;
 };
 
@@ -110,9 +130,39 @@ struct alignas(16) RowMask {
     int pad[2];
 };
 
+// The accumulators of a warp's 8 query rows from the 4-bit pages' order of d (lane g, register i: d = (D/8) g + i) to the mma's
+// own (block mb, half e: 16 mb + 8 e + g): lane bits and register bits change places, one exchange of half the registers each.
+template <int D>
+__device__ __forceinline__ void reorder(float (&O)[D / 16][4], int g) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        float v[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) v[i] = O[i >> 1][(i & 1) * 2 + n];
+#pragma unroll
+        for (int bit = 0; bit < 3; ++bit) {
+            const bool up = (g >> bit) & 1;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+                if (!((i >> bit) & 1)) {
+                    const int j = i | 1 << bit;
+                    const float got = __shfl_xor_sync(0xffffffffu, up ? v[i] : v[j], 4 << bit);
+                    if (up) v[i] = got;
+                    else v[j] = got;
+                }
+        }
+        // register bits now: the lowest three are the lane's old ones
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            if constexpr (D == 128) O[i & 7][(i >> 3) * 2 + n] = v[i];
+            else O[i >> 1][(i & 1) * 2 + n] = v[i];
+        }
+    }
+}
+
 // One 16-key tile's softmax and the probabilities as the second product's B operand.  c: scores [key g | g + 8][rows 2t, 2t+1].
-template <bool HALF>
-__device__ __forceinline__ void softmax_tile(float (&c)[4], float (&m)[2], float (&l)[2], float s0, float s1, bool two, uint32_t (&b)[2],
+template <bool HALF, bool TWO>
+__device__ __forceinline__ void softmax_tile(float (&c)[4], float (&m)[2], float (&l)[2], float s0, float s1, uint32_t (&b)[2],
                                              uint32_t (&blo)[2], bool &raise, float (&f)[2]) {
     c[0] *= s0; c[1] *= s1; c[2] *= s0; c[3] *= s1;
     float x0 = fmaxf(c[0], c[2]), x1 = fmaxf(c[1], c[3]);
@@ -136,52 +186,63 @@ __device__ __forceinline__ void softmax_tile(float (&c)[4], float (&m)[2], float
     const uint32_t h0 = pack2<HALF>(c[0], c[1]), h1 = pack2<HALF>(c[2], c[3]);
     b[0] = transpose8(h0);
     b[1] = transpose8(h1);
-    if (two) {
+    if constexpr (TWO) {
         const float2 v0 = unpack2<HALF>(h0), v1 = unpack2<HALF>(h1);
         blo[0] = transpose8(pack2<HALF>(c[0] - v0.x, c[1] - v0.y));
         blo[1] = transpose8(pack2<HALF>(c[2] - v1.x, c[3] - v1.y));
     }
 }
 
-template <int D, int NB>
-__global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel(const __grid_constant__ CUtensorMap map_kv, AttnParams p, int share) {
+// TWO: queries (and outputs) in two bf16 terms, and then probabilities of 4-bit pages in two fp16 terms
+template <int D, int NB, bool TWO>
+__global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const __grid_constant__ CUtensorMap map_kv, AttnParams p) {
     using F = Few<D, NB>;
-    constexpr int KS = D / 16, MB = D / 16;
+    constexpr int KS = D / 16, MB = D / 16, kWarps = F::WARPS;
+    constexpr int CH = NB == 1 ? 4 : 2;                      // independent sums of the first product (its chain of mma would wait for itself)
     extern __shared__ unsigned char smem_raw[];
-    unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    unsigned char *ring = smem, *sQ = smem + F::Q_AT;
+    unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);       // (an offset: the pointer stays a shared one)
+    unsigned char *sQ = smem + F::Q_AT;
     float *red = reinterpret_cast<float *>(smem + F::RED_AT);
-    __shared__ FewBars<F::SLOTS> bars;
+    __shared__ FewBars<F::TEAMS, F::SLOTS> bars;
     __shared__ int upto[kMaxSeqs + 1];                       // pages (of all heads) of the sequences before
+    __shared__ int lens[kMaxSeqs], helds[kMaxSeqs];          // positions; pages held in 4 bits
+    __shared__ int most_pages[32];                           // of a (sequence, kv head)
     __shared__ RowMask mask[8 * NB];
-    __shared__ float red_m[kWarps][8], red_l[kWarps][8];
+    __shared__ int pages[F::TEAMS][32];
+    __shared__ float red_m[kWarps][8 * NB], red_l[kWarps][8 * NB];
 
+    // test hook: phases of the first CTA (entry, set up, predecessor done, queries staged, first page there, pages done, warps
+    // merged, part handed over, end), and the grid's span
+    unsigned long long *trace = p.trace && blockIdx.x == 0 && threadIdx.x == 0 ? p.trace : nullptr;
+    if (trace) trace[0] = global_ns();
+    if (p.trace && threadIdx.x == 0) atomicMin(p.trace + 14, (unsigned long long)global_ns());
     pdl_launch_dependents();
+    static_assert(NB <= kTeam, "the teams' sums of an item fit the warps' places");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int G = p.Hq / p.Hkv, PR = p.T * G;
     volatile int *abort_flag = &bars.abort_flag;
-    // positions that rows see, of a sequence (lengths may be read before the dependency wait: see attention_tc.cu)
-    auto pages_of = [&](int s, int &P, PageList &l) {
-        P = max(p.seq_len[s], 0);
-        l = page_list(P + p.T, window_low(P, p.window), p.sinks);
-    };
+    auto list_of = [&](int P) { return page_list(P + p.T, window_low(P, p.window), p.sinks); };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < F::SLOTS; ++i) {
-            mbar_init(&bars.full[i], 1);
-            mbar_init(&bars.empty[i], kWarps);
+        for (int i = 0; i < F::TEAMS * F::SLOTS; ++i) {
+            mbar_init(&bars.full[0][0] + i, 1);
+            mbar_init(&bars.empty[0][0] + i, kTeam);
         }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        int run = 0;
+        // lengths may be read before the dependency wait: see attention_tc.cu
+        int run = 0, most = 0;
         for (int s0 = 0; s0 < p.batch; s0 += 32) {
             int n = 0;
             if (s0 + lane < p.batch) {
-                int P;
-                PageList l;
-                pages_of(s0 + lane, P, l);
-                n = l.count * p.Hkv;
+                const int P = max(p.seq_len[s0 + lane], 0);
+                const int h = p.held_len ? min(max(p.held_len[s0 + lane], 0), P) / kPage : 0;
+                lens[s0 + lane] = P;
+                helds[s0 + lane] = h;
+                n = list_of(P).count;
+                most = max(most, n);
+                n *= p.Hkv;
             }
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -191,80 +252,129 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
             if (s0 + lane < p.batch) upto[s0 + lane + 1] = run + n;
             run += __shfl_sync(0xffffffffu, n, 31);
         }
+        most_pages[lane] = most;
         if (lane == 0) upto[0] = 0;
     }
     __syncthreads();
-    const int total = upto[p.batch];
-    // equal stretches, of `share` pages at least
-    const int chunk = max((total + (int)gridDim.x - 1) / (int)gridDim.x, share);
-    const int x_begin = min((int)blockIdx.x * chunk, total), x_end = min(x_begin + chunk, total);
-    int s = 0;
-    while (s + 1 < p.batch && upto[s + 1] <= x_begin) ++s;
+    // ---- this CTA's stretch of the line: either equal stretches, which may begin and end inside an item ((sequence, kv head)),
+    // or, where that costs the longest item no more than kEven pages, the same number of CTAs for every item, so that a CTA
+    // has one item to start and to finish (4 to 5 us each). ----
+    const int total = upto[p.batch], items = p.batch * p.Hkv;
+    int most = most_pages[lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    int chunk = (total + (int)gridDim.x - 1) / (int)gridDim.x, per_item = (int)gridDim.x / items;
+    if (per_item > 0 && (most + per_item - 1) / per_item > chunk + kEven) per_item = 0;
+    int s = 0, x_begin, x_end;
+    if (per_item > 0) {
+        const int item = (int)blockIdx.x / per_item, sub = (int)blockIdx.x % per_item;
+        s = min(item / p.Hkv, p.batch - 1);
+        const int n = (upto[s + 1] - upto[s]) / p.Hkv, first = upto[s] + item % p.Hkv * n;
+        chunk = (n + per_item - 1) / per_item;
+        x_begin = first + min(sub * chunk, n);
+        x_end = item < items ? first + min((sub + 1) * chunk, n) : x_begin;
+    } else {
+        x_begin = min((int)blockIdx.x * chunk, total);
+        x_end = min(x_begin + chunk, total);
+        while (s + 1 < p.batch && upto[s + 1] <= x_begin) ++s;
+    }
 
-    if (warp == kWarps) {
-        // ---------------- producer ----------------
-        if (lane == 0) {
-            bool waited = false, ok = true;
-            int u = 0;                                       // sub-slots used so far
-            auto take = [&](int n) {                         // waits until the next n sub-slots are free
-                for (int i = 0; i < n && ok; ++i)
-                    ok = mbar_wait(&bars.empty[(u + i) % F::SLOTS], (uint32_t)(((u + i) / F::SLOTS) & 1) ^ 1u, abort_flag, p.status);
-                return ok;
+    // Page i of the CTA's stretch belongs to team i % TEAMS.
+    const int team = warp < kWarps ? warp / kTeam : warp - kWarps;
+    unsigned char *ring = smem + team * F::PLACES * F::PAGE_BYTES;
+    uint64_t *full = bars.full[team], *empty = bars.empty[team];
+    int slot = 0;                                            // of the team's ring: next to be filled or taken, and how often round
+    uint32_t phase = 0u;
+    auto advance = [&](int n) {
+        slot += n;
+        if (slot >= F::SLOTS) {
+            slot -= F::SLOTS;
+            phase ^= 1u;
+        }
+    };
+
+    if (warp >= kWarps) {
+        // ---------------- a team's producer: lane 0 issues; all lanes look up page numbers, 32 at a time and ahead ----------------
+        bool waited = false, ok = true;
+        int *numbers = pages[team];
+        for (int x = x_begin; x < x_end && ok;) {
+            while (upto[s + 1] <= x) ++s;
+            const int P = lens[s], held = helds[s];
+            const PageList list = list_of(P);
+            const int kvh = (x - upto[s]) / list.count, v0 = (x - upto[s]) % list.count;
+            const int v1 = min(list.count, v0 + (x_end - x));
+            auto look_up = [&](int v) {                      // page of entry v in its pool
+                if (v >= v1) return 0;
+                const int pg = list.page(v);
+                const size_t entry = (size_t)s * p.geom.max_pages_per_seq + pg;
+                int page = -1;
+                if (pg < p.geom.max_pages_per_seq) page = pg < held ? p.held_table[entry] : p.page_table[entry];
+                if (page < 0 || page >= (pg < held ? p.held_pages : p.geom.n_pages)) {
+                    page = 0;
+                    set_status(p.status, GLANCE_E_BOUNDS);
+                }
+                return page;
             };
-            for (int x = x_begin; x < x_end && ok;) {
-                while (upto[s + 1] <= x) ++s;
-                int P;
-                PageList list;
-                pages_of(s, P, list);
-                const int held = p.held_len ? min(max(p.held_len[s], 0), P) / kPage : 0;
-                const int kvh = (x - upto[s]) / list.count, v0 = (x - upto[s]) % list.count;
-                const int v1 = min(list.count, v0 + (x_end - x));
-                for (int v = v0; v < v1 && ok; ++v) {
-                    const int pg = list.page(v);
+            const int first = v0 + (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS;
+            int ahead = look_up(first + F::TEAMS * lane);
+            int k = 0;                                       // pages of this team in the item
+            for (int v = first; v < v1; v += F::TEAMS, ++k) {
+                if (k % 32 == 0) {
+                    numbers[lane] = ahead;
+                    ahead = look_up(v + F::TEAMS * (32 + lane));
+                    __syncwarp();
+                }
+                if (lane == 0 && ok) {
+                    const int pg = list.page(v), page = numbers[k % 32];
                     if (!waited && (pg + 1) * kPage > P - kMaxBlock) {      // rows that this pass may write
                         pdl_wait();
                         waited = true;
                     }
-                    const bool in_table = pg < p.geom.max_pages_per_seq;
-                    const size_t entry = (size_t)s * p.geom.max_pages_per_seq + pg;
                     if (pg < held) {
-                        int page = in_table ? p.held_table[entry] : -1;
-                        if (page < 0 || page >= p.held_pages) { page = 0; set_status(p.status, GLANCE_E_BOUNDS); }
-                        if (!take(1)) break;
-                        uint64_t *bar = &bars.full[u % F::SLOTS];
-                        mbar_expect_tx(bar, Tile<D>::BYTES);
-                        bulk_load(ring + (u % F::SLOTS) * F::SUB, p.held_layer + ((size_t)page * p.Hkv + kvh) * Tile<D>::BYTES, Tile<D>::BYTES, bar);
-                        u += 1;
-                    } else {
-                        int page = in_table ? p.page_table[entry] : -1;
-                        if (page < 0 || page >= p.geom.n_pages) { page = 0; set_status(p.status, GLANCE_E_BOUNDS); }
-                        const int skip = (3 - u % 3) % 3;    // to the next place for a whole bf16 page; nothing is put into these
-                        if (!take(skip + 3)) break;
-                        for (int i = 0; i < skip; ++i) mbar_arrive(&bars.full[(u + i) % F::SLOTS]);
-                        u += skip;
-                        const int at = u % F::SLOTS;
-                        mbar_arrive(&bars.full[at + 1]);
-                        mbar_arrive(&bars.full[at + 2]);
-                        mbar_expect_tx(&bars.full[at], F::PAGE_BYTES);
-#pragma unroll
-                        for (int kv = 0; kv < 2; ++kv) {
-                            const int row = ((page * 2 + kv) * p.Hkv + kvh) * kPage;
-#pragma unroll
-                            for (int sl = 0; sl < D / 64; ++sl)
-                                tma_load_2d(ring + at * F::SUB + (kv * (D / 64) + sl) * (kPage * 128), &map_kv, &bars.full[at], sl * 64, row);
+                        ok = mbar_wait(&empty[slot], phase ^ 1u, abort_flag, p.status);
+                        if (ok) {
+                            mbar_expect_tx(&full[slot], Tile<D>::BYTES);
+                            bulk_load(ring + slot / 3 * F::PAGE_BYTES + slot % 3 * F::THIRD,
+                                      p.held_layer + ((size_t)page * p.Hkv + kvh) * Tile<D>::BYTES, Tile<D>::BYTES, &full[slot]);
+                            advance(1);
                         }
-                        u += 3;
+                    } else {
+                        while (ok && slot % 3) {             // on to the next place for a whole bf16 page; nothing is put into these
+                            ok = mbar_wait(&empty[slot], phase ^ 1u, abort_flag, p.status);
+                            if (ok) {
+                                mbar_arrive(&full[slot]);
+                                advance(1);
+                            }
+                        }
+                        for (int i = 0; i < 3 && ok; ++i) ok = mbar_wait(&empty[slot + i], phase ^ 1u, abort_flag, p.status);
+                        if (ok) {
+                            mbar_arrive(&full[slot + 1]);
+                            mbar_arrive(&full[slot + 2]);
+                            mbar_expect_tx(&full[slot], F::PAGE_BYTES);
+                            unsigned char *dst = ring + slot / 3 * F::PAGE_BYTES;
+#pragma unroll
+                            for (int kv = 0; kv < 2; ++kv) {
+                                const int row = ((page * 2 + kv) * p.Hkv + kvh) * kPage;
+#pragma unroll
+                                for (int sl = 0; sl < D / 64; ++sl)
+                                    tma_load_2d(dst + (kv * (D / 64) + sl) * (kPage * 128), &map_kv, &full[slot], sl * 64, row);
+                            }
+                            advance(3);
+                        }
                     }
                 }
-                x += v1 - v0;
+                if (k % 32 == 31) __syncwarp();              // the page numbers are no longer read
             }
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            x += v1 - v0;
+        }
+        if (lane == 0) {
             if (!waited) pdl_wait();
             if (*abort_flag) {                               // copies already issued must land before the CTA may exit
                 for (int i = 0; i < F::SLOTS; ++i) {
-                    const int w = u - 1 - i;
-                    if (w < 0) break;
+                    // the latest use of slot i: in this round of the ring if it lies before `slot`, else in the last one
                     const uint64_t t0 = global_ns();
-                    while (!mbar_try_wait(&bars.full[w % F::SLOTS], (uint32_t)(w / F::SLOTS) & 1u))
+                    while (!mbar_try_wait(&full[i], i < slot ? phase : phase ^ 1u))
                         if (global_ns() - t0 > kWaitLimitNs) break;
                 }
             }
@@ -274,22 +384,21 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
     }
 
     // ---------------- consumers ----------------
+    if (trace) trace[1] = global_ns();
     pdl_wait();
+    if (trace) trace[2] = global_ns();
     const int g = lane >> 2, t = lane & 3, tid = threadIdx.x;
     const float sl2 = rsqrtf((float)D) * 1.4426950408889634f;
-    const int kA = warp * 16 + key_of(g);                    // this lane's keys as rows of K: kA, kA + 8
-    const int kV0 = warp * 16 + t, kV1 = warp * 16 + 4 + (t ^ 1);      // and as columns of V^T: kV0, kV1, kV0 + 8, kV1 + 8
-    const bool two = p.q_lo != nullptr;
-    int u = 0;
+    const int first_key = warp % kTeam * 16;
+    const int kA = first_key + key_of(g);                    // this lane's keys as rows of K: kA, kA + 8
+    const int kV0 = first_key + t, kV1 = first_key + 4 + (t ^ 1);      // and as columns of V^T: kV0, kV1, kV0 + 8, kV1 + 8
     bool ok = true;
 
     // (a warp whose wait gave up takes no more pages, but goes through every barrier and counts its items in)
     for (int x = x_begin; x < x_end;) {
         while (upto[s + 1] <= x) ++s;
-        int P;
-        PageList list;
-        pages_of(s, P, list);
-        const int held = p.held_len ? min(max(p.held_len[s], 0), P) / kPage : 0;
+        const int P = lens[s], held = helds[s];
+        const PageList list = list_of(P);
         const int kvh = (x - upto[s]) / list.count, v0 = (x - upto[s]) % list.count;
         const int v1 = min(list.count, v0 + (x_end - x));
         const int n_keys = P + p.T;
@@ -297,8 +406,8 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
         const int low_max = p.window > 0 ? window_low(P + p.T - 1, p.window) : low_min;       // every row does
 
         // ---- the item's queries and what they see ----
-        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");      // the previous item's are no longer read
-        for (int r = tid; r < 8 * NB; r += kWarps * 32) {
+        if (x > x_begin) asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");      // the previous item's are no longer read
+        for (int r = tid - (kWarps - 1) * 32; r >= 0 && r < 8 * NB; r += 32) {
             RowMask rm;
             rm.low = 0x7fffffff;                             // rows that do not exist see nothing
             rm.bits[0] = rm.bits[1] = rm.bits[2] = rm.bits[3] = 0;
@@ -314,17 +423,38 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
         }
         {
             constexpr int E = D / 32;                        // elements of a row that a lane stages: E * lane ..
-            for (int r = warp; r < 8 * NB; r += kWarps) {
-                float hi[E], lo[E];
+            constexpr int NR = (8 * NB + kWarps - 1) / kWarps;     // rows of a warp, all in flight together
+            uint32_t raw[NR][E / 2], raw_lo[NR][E / 2];
 #pragma unroll
-                for (int e = 0; e < E; ++e) hi[e] = lo[e] = 0.f;
+            for (int k = 0; k < NR; ++k) {
+                const int r = warp + k * kWarps;
+#pragma unroll
+                for (int e = 0; e < E / 2; ++e) raw[k][e] = raw_lo[k][e] = 0u;
                 if (r < PR) {
                     const size_t off = ((size_t)(s * p.T + r / G) * p.Hq + kvh * G + r % G) * D + lane * E;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        hi[e] = __bfloat162float(p.q[off + e]);
-                        if (two) lo[e] = __bfloat162float(p.q_lo[off + e]);
+                    if constexpr (E == 4) {
+                        const uint2 v = *reinterpret_cast<const uint2 *>(p.q + off);
+                        raw[k][0] = v.x; raw[k][1] = v.y;
+                        if constexpr (TWO) {
+                            const uint2 w = *reinterpret_cast<const uint2 *>(p.q_lo + off);
+                            raw_lo[k][0] = w.x; raw_lo[k][1] = w.y;
+                        }
+                    } else {
+                        raw[k][0] = *reinterpret_cast<const uint32_t *>(p.q + off);
+                        if (TWO) raw_lo[k][0] = *reinterpret_cast<const uint32_t *>(p.q_lo + off);
                     }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < NR; ++k) {
+                const int r = warp + k * kWarps;
+                if (8 * NB % kWarps && r >= 8 * NB) break;
+                float hi[E], lo[E];
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const float2 v = unpack2<false>(raw[k][e / 2]), w = unpack2<false>(raw_lo[k][e / 2]);
+                    hi[e] = v.x; hi[e + 1] = v.y;
+                    lo[e] = w.x; lo[e + 1] = w.y;
                 }
                 float top = 0.f;
 #pragma unroll
@@ -367,6 +497,7 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
         }
         asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
 
+        if (trace) trace[3] = global_ns();
         float O[NB][MB][4], m[NB][2], l[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -399,32 +530,21 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
                 O[nb][mb][0] *= f[0]; O[nb][mb][1] *= f[1]; O[nb][mb][2] *= f[0]; O[nb][mb][3] *= f[1];
             }
         };
-        // O's rows: 4-bit pages: row g of block mb is d = (D/8) g + 2 mb, row g + 8 the next one; bf16 pages: 16 mb + g, + 8
-        bool order4 = false;
-        auto to_memory = [&](int nb, bool from4, float *dst) {       // dst [8 rows][ROWF]
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                const int d0 = from4 ? (D / 8) * g + 2 * mb : 16 * mb + g, d1 = from4 ? d0 + 1 : d0 + 8;
-                dst[(2 * t) * F::ROWF + d0] = O[nb][mb][0];
-                dst[(2 * t + 1) * F::ROWF + d0] = O[nb][mb][1];
-                dst[(2 * t) * F::ROWF + d1] = O[nb][mb][2];
-                dst[(2 * t + 1) * F::ROWF + d1] = O[nb][mb][3];
-            }
-        };
-
-        for (int v = v0; v < v1 && ok; ++v) {
-            const int pg = list.page(v), key0 = pg * kPage;
-            const bool open = key0 + kPage <= P && (key0 + kPage <= p.sinks || key0 >= low_max);     // every row sees all of it
-            if (pg < held) {
-                // ---------------- a page in 4 bits ----------------
-                order4 = true;
-                ok = mbar_wait(&bars.full[u % F::SLOTS], (uint32_t)(u / F::SLOTS) & 1u, abort_flag, p.status);
+        // ---------------- pages in 4 bits: a prefix of the stretch's entries ----------------
+        const int n_held = min(max(held <= list.head ? held : list.head + max(held - max(list.next, list.head), 0), v0), v1) - v0;
+        bool order4 = false;                                 // the accumulators have the 4-bit pages' order of d
+        int i = (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS;     // this team's first entry
+        {
+            for (; i < n_held; i += F::TEAMS) {
+                const int pg = list.page(v0 + i), key0 = pg * kPage;
+                const bool open = key0 + kPage <= p.sinks || key0 >= low_max;        // every row sees all of it (it lies below P)
+                if (ok) ok = mbar_wait(&full[slot], phase, abort_flag, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const unsigned char *tile = ring + (u % F::SLOTS) * F::SUB;
-                float c[NB][4];
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) c[nb][0] = c[nb][1] = c[nb][2] = c[nb][3] = 0.f;
+                if (trace && !order4) trace[4] = global_ns();
+                order4 = true;
+                const unsigned char *tile = ring + slot / 3 * F::PAGE_BYTES + slot % 3 * F::THIRD;
+                float cc[CH][NB][4];
                 {
                     constexpr int WORDS = D / 32;            // words of a key that a lane takes: d = (D/4) t ..
                     uint32_t wa[WORDS], wb[WORDS], sa, sb;
@@ -453,20 +573,22 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
                         codes_to_half(wa[w], ha);
                         codes_to_half(wb[w], hb);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            ha[i] = mul_half2(ha[i], ga);
-                            hb[i] = mul_half2(hb[i], gb);
+                        for (int k = 0; k < 4; ++k) {
+                            ha[k] = mul_half2(ha[k], ga);
+                            hb[k] = mul_half2(hb[k], gb);
                         }
                         const uint32_t a0[4] = {ha[0], hb[0], ha[1], hb[1]}, a1[4] = {ha[2], hb[2], ha[3], hb[3]};
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) {
                             const uint4 q = *reinterpret_cast<const uint4 *>(sQ + nb * F::QB + (w * 32 + lane) * 16);
-                            mma<true>(c[nb], a0, q.x, q.y);
-                            mma<true>(c[nb], a1, q.z, q.w);
-                            if (two) {
+                            if (2 * w < CH) mma_first<true>(cc[2 * w % CH][nb], a0, q.x, q.y);
+                            else mma<true>(cc[2 * w % CH][nb], a0, q.x, q.y);
+                            if (2 * w < CH) mma_first<true>(cc[(2 * w + 1) % CH][nb], a1, q.z, q.w);
+                            else mma<true>(cc[(2 * w + 1) % CH][nb], a1, q.z, q.w);
+                            if constexpr (TWO) {
                                 const uint4 ql = *reinterpret_cast<const uint4 *>(sQ + (NB + nb) * F::QB + (w * 32 + lane) * 16);
-                                mma<true>(c[nb], a0, ql.x, ql.y);
-                                mma<true>(c[nb], a1, ql.z, ql.w);
+                                mma<true>(cc[2 * w % CH][nb], a0, ql.x, ql.y);
+                                mma<true>(cc[(2 * w + 1) % CH][nb], a1, ql.z, ql.w);
                             }
                         }
                     }
@@ -474,11 +596,17 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
                 uint32_t b[NB][2], blo[NB][2];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
+                    float (&c)[4] = cc[0][nb];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (CH == 4) c[e] = (c[e] + cc[1][nb][e]) + (cc[2][nb][e] + cc[3][nb][e]);
+                        else c[e] += cc[1][nb][e];
+                    }
                     const float s0 = mask[nb * 8 + 2 * t].scale16, s1 = mask[nb * 8 + 2 * t + 1].scale16;
-                    if (!open) hide(c[nb], nb, key0);
+                    if (!open) hide(c, nb, key0);
                     bool raise;
                     float f[2];
-                    softmax_tile<true>(c[nb], m[nb], l[nb], s0, s1, two, b[nb], blo[nb], raise, f);
+                    softmax_tile<true, TWO>(c, m[nb], l[nb], s0, s1, b[nb], blo[nb], raise, f);
                     if (raise) raise_acc(nb, f);
                 }
                 {
@@ -509,53 +637,47 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
                         codes_to_half((w[2][wi] & LOW) | ((w[3][wi] << 4) & ~LOW), e23);
                         codes_to_half(((w[2][wi] >> 4) & LOW) | (w[3][wi] & ~LOW), o23);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t a[4] = {mul_half2(e01[i], s01), mul_half2(o01[i], s01), mul_half2(e23[i], s23), mul_half2(o23[i], s23)};
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t a[4] = {mul_half2(e01[k], s01), mul_half2(o01[k], s01), mul_half2(e23[k], s23), mul_half2(o23[k], s23)};
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb) {
-                                mma<true>(O[nb][wi * 4 + i], a, b[nb][0], b[nb][1]);
-                                if (two) mma<true>(O[nb][wi * 4 + i], a, blo[nb][0], blo[nb][1]);
+                                mma<true>(O[nb][wi * 4 + k], a, b[nb][0], b[nb][1]);
+                                if constexpr (TWO) mma<true>(O[nb][wi * 4 + k], a, blo[nb][0], blo[nb][1]);
                             }
                         }
                     }
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.empty[u % F::SLOTS]);
-                u += 1;
-            } else {
-                // ---------------- a page in bf16 ----------------
-                for (; u % 3; ++u) {                         // the producer's way to the next place for a whole page
-                    ok = ok && mbar_wait(&bars.full[u % F::SLOTS], (uint32_t)(u / F::SLOTS) & 1u, abort_flag, p.status);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (lane == 0) mbar_arrive(&bars.empty[u % F::SLOTS]);
+                if (lane == 0) mbar_arrive(&empty[slot]);
+                advance(1);
+            }
+        }
+        // ---------------- pages in bf16 ----------------
+        if (ok && i < v1 - v0) {
+            while (ok && slot % 3) {                         // the producer's way to the next whole place
+                ok = mbar_wait(&full[slot], phase, abort_flag, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (ok) {
+                    if (lane == 0) mbar_arrive(&empty[slot]);
+                    advance(1);
                 }
-                ok = ok && mbar_wait(&bars.full[u % F::SLOTS], (uint32_t)(u / F::SLOTS) & 1u, abort_flag, p.status);
+            }
+            if (order4) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) reorder<D>(O[nb], g);
+                order4 = false;
+            }
+            for (; i < v1 - v0; i += F::TEAMS) {
+                const int pg = list.page(v0 + i), key0 = pg * kPage;
+                const bool open = key0 + kPage <= P && (key0 + kPage <= p.sinks || key0 >= low_max);     // every row sees all of it
+                if (ok) ok = mbar_wait(&full[slot], phase, abort_flag, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (order4) {                                // the accumulators so far to this page's order
-                    order4 = false;
-                    float *mine = red + warp * 8 * F::ROWF;
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        to_memory(nb, true, mine);
-                        __syncwarp();
-#pragma unroll
-                        for (int mb = 0; mb < MB; ++mb) {
-                            const int d0 = 16 * mb + g;
-                            O[nb][mb][0] = mine[(2 * t) * F::ROWF + d0];
-                            O[nb][mb][1] = mine[(2 * t + 1) * F::ROWF + d0];
-                            O[nb][mb][2] = mine[(2 * t) * F::ROWF + d0 + 8];
-                            O[nb][mb][3] = mine[(2 * t + 1) * F::ROWF + d0 + 8];
-                        }
-                        __syncwarp();
-                    }
-                }
-                const uint32_t kbase = smem_u32(ring + (u % F::SLOTS) * F::SUB), vbase = kbase + kPage * D * 2;
-                float c[NB][4];
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) c[nb][0] = c[nb][1] = c[nb][2] = c[nb][3] = 0.f;
+                if (trace && n_held == 0 && i < F::TEAMS) trace[4] = global_ns();
+                const uint32_t kbase = smem_u32(ring + slot / 3 * F::PAGE_BYTES), vbase = kbase + kPage * D * 2;
+                float cc[CH][NB][4];
                 // lane's row of the four 8 x 8 matrices it addresses
-                const int mi = lane >> 3, r = warp * 16 + key_of(lane & 7);
+                const int mi = lane >> 3, r = first_key + key_of(lane & 7);
 #pragma unroll
                 for (int j = 0; j < KS; ++j) {
                     // keys 0-7 | 8-15 of d 0-7, then of d 8-15
@@ -565,20 +687,27 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         const uint2 q = *reinterpret_cast<const uint2 *>(sQ + (2 * NB + nb) * F::QB + ((j >> 1) * 32 + lane) * 16 + (j & 1) * 8);
-                        mma<false>(c[nb], a, q.x, q.y);
-                        if (two) {
+                        if (j < CH) mma_first<false>(cc[j % CH][nb], a, q.x, q.y);
+                        else mma<false>(cc[j % CH][nb], a, q.x, q.y);
+                        if constexpr (TWO) {
                             const uint2 ql = *reinterpret_cast<const uint2 *>(sQ + (3 * NB + nb) * F::QB + ((j >> 1) * 32 + lane) * 16 + (j & 1) * 8);
-                            mma<false>(c[nb], a, ql.x, ql.y);
+                            mma<false>(cc[j % CH][nb], a, ql.x, ql.y);
                         }
                     }
                 }
                 uint32_t b[NB][2], blo[NB][2];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    if (!open) hide(c[nb], nb, key0);
+                    float (&c)[4] = cc[0][nb];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (CH == 4) c[e] = (c[e] + cc[1][nb][e]) + (cc[2][nb][e] + cc[3][nb][e]);
+                        else c[e] += cc[1][nb][e];
+                    }
+                    if (!open) hide(c, nb, key0);
                     bool raise;
                     float f[2];
-                    softmax_tile<false>(c[nb], m[nb], l[nb], sl2, sl2, true, b[nb], blo[nb], raise, f);
+                    softmax_tile<false, true>(c, m[nb], l[nb], sl2, sl2, b[nb], blo[nb], raise, f);
                     if (raise) raise_acc(nb, f);
                 }
                 uint32_t keep01 = ~0u, keep23 = ~0u;         // what nobody sees may be anything, NaN included
@@ -600,16 +729,18 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
                     }
                 }
                 __syncwarp();
-                if (lane < 3) mbar_arrive(&bars.empty[u % F::SLOTS + lane]);
-                u += 3;
+                if (lane < 3) mbar_arrive(&empty[slot + lane]);
+                advance(3);
             }
         }
 
+        if (trace) trace[5] = global_ns();
         // ---- the warps' parts meet; this CTA's part of the item, or all of it ----
         const int item = s * p.Hkv + kvh;
         const int first_x = x - v0, last_x = first_x + list.count - 1;       // the item's places in the line
-        const int c_first = first_x / chunk, c_last = last_x / chunk, parts = c_last - c_first + 1;
-        const int slot = 2 * (int)blockIdx.x + (first_x > x_begin ? 1 : 0);  // a CTA shares its first item, its last, or both
+        const int c_first = per_item > 0 ? (s * p.Hkv + kvh) * per_item : first_x / chunk;
+        const int parts = per_item > 0 ? (list.count + chunk - 1) / chunk : last_x / chunk - c_first + 1;
+        const int part = 2 * (int)blockIdx.x + (first_x > x_begin ? 1 : 0);  // a CTA shares its first item, its last, or both
         const int rows = min(PR, 8 * NB);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -617,68 +748,174 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int o = 4; o <= 16; o <<= 1) l[nb][r] += __shfl_xor_sync(0xffffffffu, l[nb][r], o);
-            to_memory(nb, order4, red + warp * 8 * F::ROWF);
             if (g == 0) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    red_m[warp][2 * t + r] = m[nb][r];
-                    red_l[warp][2 * t + r] = l[nb][r];
+                    red_m[warp][nb * 8 + 2 * t + r] = m[nb][r];
+                    red_l[warp][nb * 8 + 2 * t + r] = l[nb][r];
                 }
             }
-            asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-            for (int i = tid; i < 8 * (D / 4); i += kWarps * 32) {
-                const int r = i / (D / 4), d0 = i % (D / 4) * 4, row = nb * 8 + r;
-                float M = -INFINITY, L = 0.f;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red_m[w][r]);
-                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float f = red_m[w][r] == -INFINITY ? 0.f : ex2(red_m[w][r] - M);
-                    const float4 a = *reinterpret_cast<const float4 *>(red + (w * 8 + r) * F::ROWF + d0);
-                    L += f * red_l[w][r];
-                    acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
-                }
-                if (row < rows) {
-                    if (parts == 1) {
-                        const float inv = L > 0.f ? 1.f / L : 0.f;
-                        const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
-                        store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-                    } else {
-                        *reinterpret_cast<float4 *>(p.parts + ((size_t)slot * kFewRows + row) * D + d0) = acc;
-                        if (d0 == 0) reinterpret_cast<float2 *>(p.parts_ml)[(size_t)slot * kFewRows + row] = make_float2(M, L);
-                    }
-                }
-            }
-            asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
         }
+        auto put = [&](int nb, float *dst) {                 // this warp's accumulators of 8 rows to dst [8][ROWF]
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                const int d0 = order4 ? (D / 8) * g + 2 * mb : 16 * mb + g, d1 = order4 ? d0 + 1 : d0 + 8;
+                dst[(2 * t) * F::ROWF + d0] = O[nb][mb][0];
+                dst[(2 * t + 1) * F::ROWF + d0] = O[nb][mb][1];
+                dst[(2 * t) * F::ROWF + d1] = O[nb][mb][2];
+                dst[(2 * t + 1) * F::ROWF + d1] = O[nb][mb][3];
+            }
+        };
+        // element (row, d0 .. d0 + 3) over the warps w0 .. w0 + n - 1, whose accumulators lie `step` floats apart from src on
+        auto add_warps = [&](const float *src, int step, int w0, int n, int row, int d0, float M, float4 &acc, float &L) {
+#pragma unroll 4
+            for (int w = 0; w < n; ++w) {
+                const float mw = red_m[w0 + w][row], f = mw == -INFINITY ? 0.f : ex2(mw - M);
+                const float4 a = *reinterpret_cast<const float4 *>(src + w * step + (row & 7) * F::ROWF + d0);
+                L += f * red_l[w0 + w][row];
+                acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
+            }
+        };
+        auto top_of = [&](int row) {
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, red_m[w][row]);
+            return M;
+        };
+        auto emit = [&](int row, int d0, float M, float L, float4 acc) {
+            if (row >= rows) return;
+            if (parts == 1) {
+                const float inv = L > 0.f ? 1.f / L : 0.f;
+                const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
+                store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+            } else {
+                *reinterpret_cast<float4 *>(p.parts + ((size_t)part * kFewRows + row) * D + d0) = acc;
+                if (d0 == 0) reinterpret_cast<float2 *>(p.parts_ml)[(size_t)part * kFewRows + row] = make_float2(M, L);
+            }
+        };
+        constexpr int ELEMS = 8 * (D / 4), WARP_F = 8 * F::ROWF;             // of 8 rows
+        if (x + (v1 - v0) == x_end) {
+            // The CTA's last item: no more pages come, so the rings hold the accumulators of all warps and blocks at once.
+            asm volatile("bar.sync %0, %1;" ::"r"(2 + team), "n"(kTeam * 32) : "memory");        // the team has read its last page
+            float *mine = reinterpret_cast<float *>(ring);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) put(nb, mine + (nb * kTeam + warp % kTeam) * WARP_F);
+            asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+            for (int i = tid; i < NB * ELEMS; i += kWarps * 32) {
+                const int nb = i / ELEMS, row = nb * 8 + i % ELEMS / (D / 4), d0 = i % (D / 4) * 4;
+                const float M = top_of(row);
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                float L = 0.f;
+#pragma unroll
+                for (int k = 0; k < F::TEAMS; ++k)
+                    add_warps(reinterpret_cast<const float *>(smem + k * F::PLACES * F::PAGE_BYTES) + nb * kTeam * WARP_F, WARP_F, k * kTeam, kTeam, row, d0, M, acc, L);
+                emit(row, d0, M, L, acc);
+            }
+        } else {
+            // pages of the next item are under way: one team and block at a time, a thread keeps its element's sum over the teams
+            constexpr int PER = (ELEMS + kWarps * 32 - 1) / (kWarps * 32);
+            for (int nb = 0; nb < NB; ++nb) {
+                float4 acc[PER];
+                float M[PER], L[PER];
+                for (int k = 0; k < F::TEAMS; ++k) {
+                    if (team == k) {
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+                            if (b == nb) put(b, red + warp % kTeam * WARP_F);
+                    }
+                    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) {
+                        const int i = tid + e * kWarps * 32, row = nb * 8 + i / (D / 4), d0 = i % (D / 4) * 4;
+                        if (i >= ELEMS) break;
+                        if (k == 0) {
+                            M[e] = top_of(row);
+                            L[e] = 0.f;
+                            acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
+                        add_warps(red, WARP_F, k * kTeam, kTeam, row, d0, M[e], acc[e], L[e]);
+                        if (k == F::TEAMS - 1) emit(row, d0, M[e], L[e], acc[e]);
+                    }
+                    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+                }
+            }
+        }
+        if (trace) trace[6] = global_ns();
         if (parts > 1) {
-            __threadfence();
             asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
             if (tid == 0) {
-                bars.last = atomicAdd(p.part_counters + item, 1) == parts - 1;
-                if (bars.last) p.part_counters[item] = 0;    // for the next launch
+                // releases what the whole CTA wrote (the barrier orders it before this thread), acquires the others' parts
+                int before;
                 __threadfence();
+                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.part_counters + item) : "memory");
+                bars.last = before == parts - 1;
+                if (bars.last) p.part_counters[item] = 0;    // for the next launch
             }
             asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+            if (trace) trace[7] = global_ns();
             if (bars.last) {
+                // every team takes every TEAMS-th part, 8 elements a thread; the teams' sums meet in shared memory
+                // (the part of the item's first CTA is its second one if another item came before)
+                const int s_first = 2 * c_first + (per_item == 0 && first_x > c_first * chunk ? 1 : 0);
+                float *team_m = &red_m[0][0], *team_l = &red_l[0][0];        // [team][8 NB]
+                for (int i = tid % (kTeam * 32); i < rows * (D / 8); i += kTeam * 32) {
+                    const int row = i / (D / 8), d0 = i % (D / 8) * 8;
+                    float M = -INFINITY, L = 0.f;
+                    float acc[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+                    constexpr int U = NB == 4 ? 12 : 7;      // parts in flight
+                    for (int c0 = team; c0 < parts; c0 += U * F::TEAMS) {
+                        float2 ml[U];
+                        float4 a[U][2];
+#pragma unroll
+                        for (int k = 0; k < U; ++k) {
+                            const int c = min(c0 + k * F::TEAMS, parts - 1);
+                            const size_t at = (size_t)(c == 0 ? s_first : 2 * (c_first + c)) * kFewRows + row;
+                            ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.parts_ml) + at);
+                            a[k][0] = __ldcg(reinterpret_cast<const float4 *>(p.parts + at * D + d0));
+                            a[k][1] = __ldcg(reinterpret_cast<const float4 *>(p.parts + at * D + d0) + 1);
+                        }
+                        float M2 = M;
+#pragma unroll
+                        for (int k = 0; k < U; ++k) {
+                            if (c0 + k * F::TEAMS >= parts) ml[k] = make_float2(-INFINITY, 0.f);
+                            M2 = fmaxf(M2, ml[k].x);
+                        }
+                        const float f0 = M == -INFINITY ? 0.f : ex2(M - M2);
+                        L *= f0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[e] *= f0;
+#pragma unroll
+                        for (int k = 0; k < U; ++k) {
+                            const float f = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - M2);
+                            L += ml[k].y * f;
+                            acc[0] += a[k][0].x * f; acc[1] += a[k][0].y * f; acc[2] += a[k][0].z * f; acc[3] += a[k][0].w * f;
+                            acc[4] += a[k][1].x * f; acc[5] += a[k][1].y * f; acc[6] += a[k][1].z * f; acc[7] += a[k][1].w * f;
+                        }
+                        M = M2;
+                    }
+                    float *dst = red + (team * 8 * NB + row) * F::ROWF + d0;
+                    *reinterpret_cast<float4 *>(dst) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                    *reinterpret_cast<float4 *>(dst + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                    if (d0 == 0) {
+                        team_m[team * 8 * NB + row] = M;
+                        team_l[team * 8 * NB + row] = L;
+                    }
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
                 for (int i = tid; i < rows * (D / 4); i += kWarps * 32) {
                     const int row = i / (D / 4), d0 = i % (D / 4) * 4;
-                    // the part of the item's first CTA is its second one if another item came before
-                    const int s_first = 2 * c_first + (first_x > c_first * chunk ? 1 : 0);
                     float M = -INFINITY, L = 0.f;
+#pragma unroll
+                    for (int k = 0; k < F::TEAMS; ++k) M = fmaxf(M, team_m[k * 8 * NB + row]);
                     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-                    for (int c = 0; c < parts; ++c) {
-                        const size_t at = (size_t)(c == 0 ? s_first : 2 * (c_first + c)) * kFewRows + row;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p.parts_ml) + at);
-                        const float4 a = __ldcg(reinterpret_cast<const float4 *>(p.parts + at * D + d0));
-                        const float M2 = fmaxf(M, ml.x);
-                        const float f0 = M == -INFINITY ? 0.f : ex2(M - M2), f1 = ml.x == -INFINITY ? 0.f : ex2(ml.x - M2);
-                        M = M2;
-                        L = L * f0 + ml.y * f1;
-                        acc.x = acc.x * f0 + a.x * f1; acc.y = acc.y * f0 + a.y * f1;
-                        acc.z = acc.z * f0 + a.z * f1; acc.w = acc.w * f0 + a.w * f1;
+#pragma unroll
+                    for (int k = 0; k < F::TEAMS; ++k) {
+                        const float mk = team_m[k * 8 * NB + row], f = mk == -INFINITY ? 0.f : ex2(mk - M);
+                        const float4 a = *reinterpret_cast<const float4 *>(red + (k * 8 * NB + row) * F::ROWF + d0);
+                        L += f * team_l[k * 8 * NB + row];
+                        acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
                     }
                     const float inv = L > 0.f ? 1.f / L : 0.f;
                     const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
@@ -688,14 +925,16 @@ __global__ void __launch_bounds__(kFewThreads, Few<D, NB>::CTAS) attn_few_kernel
         }
         x += v1 - v0;
     }
+    if (trace) trace[11] = global_ns();
+    if (p.trace && threadIdx.x == 0) atomicMax(p.trace + 15, (unsigned long long)global_ns());
 }
 
-template <int D, int NB>
+template <int D, int NB, bool TWO>
 cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
     using F = Few<D, NB>;
     static bool once = false;
     if (!once) {
-        const cudaError_t e = cudaFuncSetAttribute(attn_few_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::TOTAL);
+        const cudaError_t e = cudaFuncSetAttribute(attn_few_kernel<D, NB, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::TOTAL);
         if (e != cudaSuccess) return e;
         once = true;
     }
@@ -703,8 +942,8 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStrea
     // no more CTAs than pages that a row can see: the lengths themselves are on the device
     long long pages = p.geom.max_pages_per_seq;
     if (p.window > 0) pages = std::min(pages, ((long long)p.window + p.T + kPage - 1) / kPage + 1 + ((long long)p.sinks + kPage - 1) / kPage);
-    cfg.gridDim = dim3((unsigned)std::min<long long>(148 * F::CTAS, pages * p.Hkv * p.batch), 1, 1);
-    cfg.blockDim = dim3(kFewThreads, 1, 1);
+    cfg.gridDim = dim3((unsigned)std::min<long long>(148, pages * p.Hkv * p.batch), 1, 1);
+    cfg.blockDim = dim3(F::THREADS, 1, 1);
     cfg.dynamicSmemBytes = F::TOTAL;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -712,7 +951,7 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStrea
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_few_kernel<D, NB>, map_kv, p, 1);
+    return cudaLaunchKernelEx(&cfg, attn_few_kernel<D, NB, TWO>, map_kv, p);
 }
 
 }  // namespace
@@ -720,15 +959,16 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStrea
 bool attention_few_takes(int T, int G) { return (long long)T * G <= kFewRows; }
 
 cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
-    const int rows = p.T * (p.Hq / p.Hkv);
-    if (p.d == 128) {
-        if (rows <= 8) return launch_few<128, 1>(p, map_kv, st);
-        if (rows <= 16) return launch_few<128, 2>(p, map_kv, st);
-        return launch_few<128, 4>(p, map_kv, st);
-    }
-    if (rows <= 8) return launch_few<64, 1>(p, map_kv, st);
-    if (rows <= 16) return launch_few<64, 2>(p, map_kv, st);
-    return launch_few<64, 4>(p, map_kv, st);
+    const int rows = p.T * (p.Hq / p.Hkv), blocks = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+    auto pick = [&](auto d, auto two) {
+        constexpr int D = decltype(d)::value;
+        constexpr bool TWO = decltype(two)::value;
+        return blocks == 1 ? launch_few<D, 1, TWO>(p, map_kv, st) : blocks == 2 ? launch_few<D, 2, TWO>(p, map_kv, st) : launch_few<D, 4, TWO>(p, map_kv, st);
+    };
+    using D128 = std::integral_constant<int, 128>;
+    using D64 = std::integral_constant<int, 64>;
+    if (p.d == 128) return p.q_lo ? pick(D128{}, std::true_type{}) : pick(D128{}, std::false_type{});
+    return p.q_lo ? pick(D64{}, std::true_type{}) : pick(D64{}, std::false_type{});
 }
 
 }  // namespace glance

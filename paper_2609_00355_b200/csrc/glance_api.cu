@@ -294,6 +294,10 @@ void attention(glance_ctx *ctx, AttnParams ap) {
 void attention_cache(glance_ctx *ctx, AttnParams ap, int layer, int seq_off) {
     const glance_config &c = ctx->cfg;
     ap.trace = nullptr;
+    if (ctx->trace && ctx->trace_slots > 0) {
+        ap.trace = ctx->trace + (size_t)(ctx->trace_next % ctx->trace_slots) * 16;
+        ctx->trace_next++;
+    }
     if (ctx->held.pool) {
         ap.held_len = ctx->held.len + seq_off;
         ap.held_table = ctx->held.page_table + (size_t)seq_off * c.max_pages_per_seq;

@@ -153,7 +153,7 @@ struct AttnParams {
 };
 // few query rows over a cache read in part: at most kFewRows packed rows (T * heads of a kv head)
 constexpr int kFewRows = 32;
-constexpr int kFewParts = 2 * 2 * 148;       // partial results of a launch: two a CTA, two CTAs an SM
+constexpr int kFewParts = 2 * 148;           // partial results of a launch: two a CTA, one CTA an SM
 bool attention_few_takes(int T, int G);
 cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 // map_kv = 2-D map of the pool layer {d, n_pages*2*Hkv*64 rows}, box {64, 64}
