@@ -160,29 +160,44 @@ __device__ __forceinline__ void reorder(float (&O)[D / 16][4], int g) {
     }
 }
 
-// One 16-key tile's softmax and the probabilities as the second product's B operand.  c: scores [key g | g + 8][rows 2t, 2t+1].
+// What a lane keeps of its two query rows (2t, 2t + 1): the reference maximum (0 while the row has seen nothing), the score above
+// which it is raised (-inf then), and its share of the row sum.  Log2 units.
+struct RowState {
+    float ref[2], limit[2], sum[2];
+};
+
+// One 16-key tile's softmax and the probabilities as the second product's B operand.  c: raw scores [key g | g + 8][rows 2t, 2t + 1],
+// -inf where hidden; s: scale of each row.  True if a row's reference was raised: then everything summed so far takes the factor f.
 template <bool HALF, bool TWO>
-__device__ __forceinline__ void softmax_tile(float (&c)[4], float (&m)[2], float (&l)[2], float s0, float s1, uint32_t (&b)[2],
-                                             uint32_t (&blo)[2], bool &raise, float (&f)[2]) {
-    c[0] *= s0; c[1] *= s1; c[2] *= s0; c[3] *= s1;
-    float x0 = fmaxf(c[0], c[2]), x1 = fmaxf(c[1], c[3]);
-    raise = __any_sync(0xffffffffu, x0 > m[0] + kRaise || x1 > m[1] + kRaise);      // (m starts at -inf; a row that sees nothing stays there)
-    f[0] = f[1] = 1.f;
+__device__ __forceinline__ bool softmax_tile(float (&c)[4], RowState &st, float s0, float s1, uint32_t (&b)[2], uint32_t (&blo)[2], float (&f)[2]) {
+    float x0 = fmaxf(c[0], c[2]) * s0, x1 = fmaxf(c[1], c[3]) * s1;
+    const bool raise = __any_sync(0xffffffffu, x0 > st.limit[0] || x1 > st.limit[1]);
     if (raise) {
 #pragma unroll
         for (int o = 4; o <= 16; o <<= 1) {
             x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
             x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
         }
-        if (x0 > m[0] + kRaise) { f[0] = ex2(m[0] - x0); m[0] = x0; }
-        if (x1 > m[1] + kRaise) { f[1] = ex2(m[1] - x1); m[1] = x1; }
-        l[0] *= f[0];
-        l[1] *= f[1];
+        f[0] = f[1] = 1.f;
+        if (x0 > st.limit[0]) {
+            f[0] = st.limit[0] == -INFINITY ? 0.f : ex2(st.ref[0] - x0);
+            st.ref[0] = x0;
+            st.limit[0] = x0 + kRaise;
+        }
+        if (x1 > st.limit[1]) {
+            f[1] = st.limit[1] == -INFINITY ? 0.f : ex2(st.ref[1] - x1);
+            st.ref[1] = x1;
+            st.limit[1] = x1 + kRaise;
+        }
+        st.sum[0] *= f[0];
+        st.sum[1] *= f[1];
     }
-    const float r0 = m[0] == -INFINITY ? 0.f : m[0], r1 = m[1] == -INFINITY ? 0.f : m[1];
-    c[0] = ex2(c[0] - r0); c[1] = ex2(c[1] - r1); c[2] = ex2(c[2] - r0); c[3] = ex2(c[3] - r1);
-    l[0] += c[0] + c[2];
-    l[1] += c[1] + c[3];
+    c[0] = ex2(fmaf(c[0], s0, -st.ref[0]));
+    c[1] = ex2(fmaf(c[1], s1, -st.ref[1]));
+    c[2] = ex2(fmaf(c[2], s0, -st.ref[0]));
+    c[3] = ex2(fmaf(c[3], s1, -st.ref[1]));
+    st.sum[0] += c[0] + c[2];
+    st.sum[1] += c[1] + c[3];
     const uint32_t h0 = pack2<HALF>(c[0], c[1]), h1 = pack2<HALF>(c[2], c[3]);
     b[0] = transpose8(h0);
     b[1] = transpose8(h1);
@@ -191,6 +206,34 @@ __device__ __forceinline__ void softmax_tile(float (&c)[4], float (&m)[2], float
         blo[0] = transpose8(pack2<HALF>(c[0] - v0.x, c[1] - v0.y));
         blo[1] = transpose8(pack2<HALF>(c[2] - v1.x, c[3] - v1.y));
     }
+    return raise;
+}
+
+// shared-memory loads by address, so that a page's loads differ in their immediate offsets only
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds4(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds2(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
 }
 
 // TWO: queries (and outputs) in two bf16 terms, and then probabilities of 4-bit pages in two fp16 terms
@@ -198,7 +241,7 @@ template <int D, int NB, bool TWO>
 __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const __grid_constant__ CUtensorMap map_kv, AttnParams p) {
     using F = Few<D, NB>;
     constexpr int KS = D / 16, MB = D / 16, kWarps = F::WARPS;
-    constexpr int CH = NB == 1 ? 4 : 2;                      // independent sums of the first product (its chain of mma would wait for itself)
+    constexpr int CH = 2;                                    // independent sums of the first product (its chain of mma would wait for itself)
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);       // (an offset: the pointer stays a shared one)
     unsigned char *sQ = smem + F::Q_AT;
@@ -222,12 +265,12 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     const int G = p.Hq / p.Hkv, PR = p.T * G;
     volatile int *abort_flag = &bars.abort_flag;
     auto list_of = [&](int P) { return page_list(P + p.T, window_low(P, p.window), p.sinks); };
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < F::TEAMS * F::SLOTS; ++i) {
+    if (warp == 0) {
+        for (int i = lane; i < F::TEAMS * F::SLOTS; i += 32) {
             mbar_init(&bars.full[0][0] + i, 1);
             mbar_init(&bars.empty[0][0] + i, kTeam);
         }
-        bars.abort_flag = 0;
+        if (lane == 0) bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -393,6 +436,22 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     const int kA = first_key + key_of(g);                    // this lane's keys as rows of K: kA, kA + 8
     const int kV0 = first_key + t, kV1 = first_key + 4 + (t ^ 1);      // and as columns of V^T: kV0, kV1, kV0 + 8, kV1 + 8
     bool ok = true;
+    // the whole warp waits; false (from then on) if a wait gave up
+    auto wait_all = [&](uint64_t *bar, uint32_t parity) {
+        if (!__all_sync(0xffffffffu, ok && mbar_try_wait(bar, parity))) {
+            ok = ok && mbar_wait(bar, parity, abort_flag, p.status);
+            ok = __all_sync(0xffffffffu, ok);
+        }
+        return ok;
+    };
+    // where a lane's codes and scales lie in a 4-bit tile (keys 8 later: 8 rows on, since the exchange of pieces repeats)
+    const uint32_t ring_addr = smem_u32(ring);
+    const uint32_t at_k = D == 128 ? code_at<D>(kA, t) : code_at<D>(kA, t >> 1) + (t & 1) * 8;
+    const uint32_t at_ks = Tile<D>::SCALES + kA * Tile<D>::GROUPS + (D == 128 ? 2 * t : t);
+    const uint32_t at_v0 = Tile<D>::HALF + (D == 128 ? code_at<D>(kV0, g >> 1) + (g & 1) * 8 : code_at<D>(kV0, g >> 2) + (g & 3) * 4);
+    const uint32_t at_v1 = Tile<D>::HALF + (D == 128 ? code_at<D>(kV1, g >> 1) + (g & 1) * 8 : code_at<D>(kV1, g >> 2) + (g & 3) * 4);
+    const uint32_t at_vs0 = Tile<D>::HALF + Tile<D>::SCALES + kV0 * Tile<D>::GROUPS + (D == 128 ? g : g >> 1);
+    const uint32_t at_vs1 = Tile<D>::HALF + Tile<D>::SCALES + kV1 * Tile<D>::GROUPS + (D == 128 ? g : g >> 1);
 
     // (a warp whose wait gave up takes no more pages, but goes through every barrier and counts its items in)
     for (int x = x_begin; x < x_end;) {
@@ -498,11 +557,11 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
 
         if (trace) trace[3] = global_ns();
-        float O[NB][MB][4], m[NB][2], l[NB][2];
+        float O[NB][MB][4];
+        RowState rows_st[NB];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            m[nb][0] = m[nb][1] = -INFINITY;
-            l[nb][0] = l[nb][1] = 0.f;
+            rows_st[nb] = RowState{{0.f, 0.f}, {-INFINITY, -INFINITY}, {0.f, 0.f}};
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -538,30 +597,27 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
             for (; i < n_held; i += F::TEAMS) {
                 const int pg = list.page(v0 + i), key0 = pg * kPage;
                 const bool open = key0 + kPage <= p.sinks || key0 >= low_max;        // every row sees all of it (it lies below P)
-                if (ok) ok = mbar_wait(&full[slot], phase, abort_flag, p.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+                if (!wait_all(&full[slot], phase)) break;
                 if (trace && !order4) trace[4] = global_ns();
                 order4 = true;
-                const unsigned char *tile = ring + slot / 3 * F::PAGE_BYTES + slot % 3 * F::THIRD;
+                const uint32_t tile = ring_addr + (uint32_t)(slot / 3 * F::PAGE_BYTES + slot % 3 * F::THIRD);
                 float cc[CH][NB][4];
                 {
                     constexpr int WORDS = D / 32;            // words of a key that a lane takes: d = (D/4) t ..
                     uint32_t wa[WORDS], wb[WORDS], sa, sb;
+                    constexpr int ROW = Tile<D>::ROW, GROUPS = Tile<D>::GROUPS;
                     if constexpr (D == 128) {
-                        const uint4 a = *reinterpret_cast<const uint4 *>(tile + code_at<D>(kA, t));
-                        const uint4 b = *reinterpret_cast<const uint4 *>(tile + code_at<D>(kA + 8, t));
+                        const uint4 a = lds16(tile + at_k), b = lds16(tile + at_k + 8 * ROW);
                         wa[0] = a.x; wa[1] = a.y; wa[2] = a.z; wa[3] = a.w;
                         wb[0] = b.x; wb[1] = b.y; wb[2] = b.z; wb[3] = b.w;
-                        sa = *reinterpret_cast<const uint16_t *>(tile + Tile<D>::SCALES + kA * 8 + 2 * t);
-                        sb = *reinterpret_cast<const uint16_t *>(tile + Tile<D>::SCALES + (kA + 8) * 8 + 2 * t);
+                        sa = lds2(tile + at_ks);
+                        sb = lds2(tile + at_ks + 8 * GROUPS);
                     } else {
-                        const uint2 a = *reinterpret_cast<const uint2 *>(tile + code_at<D>(kA, t >> 1) + (t & 1) * 8);
-                        const uint2 b = *reinterpret_cast<const uint2 *>(tile + code_at<D>(kA + 8, t >> 1) + (t & 1) * 8);
+                        const uint2 a = lds8(tile + at_k), b = lds8(tile + at_k + 8 * ROW);
                         wa[0] = a.x; wa[1] = a.y;
                         wb[0] = b.x; wb[1] = b.y;
-                        sa = tile[Tile<D>::SCALES + kA * 4 + t] * 0x101u;
-                        sb = tile[Tile<D>::SCALES + (kA + 8) * 4 + t] * 0x101u;
+                        sa = lds1(tile + at_ks) * 0x101u;
+                        sb = lds1(tile + at_ks + 8 * GROUPS) * 0x101u;
                     }
                     sa = scales_to_half(sa);
                     sb = scales_to_half(sb);
@@ -599,32 +655,31 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                     float (&c)[4] = cc[0][nb];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if constexpr (CH == 4) c[e] = (c[e] + cc[1][nb][e]) + (cc[2][nb][e] + cc[3][nb][e]);
-                        else c[e] += cc[1][nb][e];
+                        c[e] += cc[1][nb][e];
                     }
                     const float s0 = mask[nb * 8 + 2 * t].scale16, s1 = mask[nb * 8 + 2 * t + 1].scale16;
                     if (!open) hide(c, nb, key0);
-                    bool raise;
                     float f[2];
-                    softmax_tile<true, TWO>(c, m[nb], l[nb], s0, s1, b[nb], blo[nb], raise, f);
-                    if (raise) raise_acc(nb, f);
+                    if (softmax_tile<true, TWO>(c, rows_st[nb], s0, s1, b[nb], blo[nb], f)) raise_acc(nb, f);
                 }
                 {
-                    const unsigned char *vt = tile + Tile<D>::HALF;
                     constexpr int WORDS = D / 64;            // words of a key that a lane takes: d = (D/8) g ..
+                    constexpr int ROW = Tile<D>::ROW, GROUPS = Tile<D>::GROUPS;
                     uint32_t w[4][WORDS], sc[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int key = ((k & 1) ? kV1 : kV0) + (k >> 1) * 8;
+                    for (int k = 0; k < 4; ++k) {            // keys kV0, kV1, kV0 + 8, kV1 + 8
+                        const uint32_t at = tile + ((k & 1) ? at_v1 : at_v0) + (k >> 1) * 8 * ROW, ats = tile + ((k & 1) ? at_vs1 : at_vs0) + (k >> 1) * 8 * GROUPS;
                         if constexpr (D == 128) {
-                            const uint2 a = *reinterpret_cast<const uint2 *>(vt + code_at<D>(key, g >> 1) + (g & 1) * 8);
+                            const uint2 a = lds8(at);
                             w[k][0] = a.x; w[k][1] = a.y;
-                            sc[k] = vt[Tile<D>::SCALES + key * 8 + g];
                         } else {
-                            w[k][0] = *reinterpret_cast<const uint32_t *>(vt + code_at<D>(key, g >> 2) + (g & 3) * 4);
-                            sc[k] = vt[Tile<D>::SCALES + key * 4 + (g >> 1)];
+                            w[k][0] = lds4(at);
                         }
-                        if (!open && !see(key0 + key)) sc[k] = 0;      // what nobody sees may be anything, NaN included
+                        sc[k] = lds1(ats);
+                    }
+                    if (!open) {                             // what nobody sees may be anything, NaN included
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sc[k] = see(key0 + ((k & 1) ? kV1 : kV0) + (k >> 1) * 8) ? sc[k] : 0u;
                     }
                     const uint32_t s01 = scales_to_half(sc[0] | sc[1] << 8), s23 = scales_to_half(sc[2] | sc[3] << 8);
 #pragma unroll
@@ -655,9 +710,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         // ---------------- pages in bf16 ----------------
         if (ok && i < v1 - v0) {
             while (ok && slot % 3) {                         // the producer's way to the next whole place
-                ok = mbar_wait(&full[slot], phase, abort_flag, p.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (ok) {
+                if (wait_all(&full[slot], phase)) {
                     if (lane == 0) mbar_arrive(&empty[slot]);
                     advance(1);
                 }
@@ -670,9 +723,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
             for (; i < v1 - v0; i += F::TEAMS) {
                 const int pg = list.page(v0 + i), key0 = pg * kPage;
                 const bool open = key0 + kPage <= P && (key0 + kPage <= p.sinks || key0 >= low_max);     // every row sees all of it
-                if (ok) ok = mbar_wait(&full[slot], phase, abort_flag, p.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+                if (!wait_all(&full[slot], phase)) break;
                 if (trace && n_held == 0 && i < F::TEAMS) trace[4] = global_ns();
                 const uint32_t kbase = smem_u32(ring + slot / 3 * F::PAGE_BYTES), vbase = kbase + kPage * D * 2;
                 float cc[CH][NB][4];
@@ -701,14 +752,11 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                     float (&c)[4] = cc[0][nb];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if constexpr (CH == 4) c[e] = (c[e] + cc[1][nb][e]) + (cc[2][nb][e] + cc[3][nb][e]);
-                        else c[e] += cc[1][nb][e];
+                        c[e] += cc[1][nb][e];
                     }
                     if (!open) hide(c, nb, key0);
-                    bool raise;
                     float f[2];
-                    softmax_tile<false, true>(c, m[nb], l[nb], sl2, sl2, b[nb], blo[nb], raise, f);
-                    if (raise) raise_acc(nb, f);
+                    if (softmax_tile<false, true>(c, rows_st[nb], sl2, sl2, b[nb], blo[nb], f)) raise_acc(nb, f);
                 }
                 uint32_t keep01 = ~0u, keep23 = ~0u;         // what nobody sees may be anything, NaN included
                 if (!open) {
@@ -747,23 +795,30 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int o = 4; o <= 16; o <<= 1) l[nb][r] += __shfl_xor_sync(0xffffffffu, l[nb][r], o);
+                for (int o = 4; o <= 16; o <<= 1) rows_st[nb].sum[r] += __shfl_xor_sync(0xffffffffu, rows_st[nb].sum[r], o);
             if (g == 0) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    red_m[warp][nb * 8 + 2 * t + r] = m[nb][r];
-                    red_l[warp][nb * 8 + 2 * t + r] = l[nb][r];
+                    red_m[warp][nb * 8 + 2 * t + r] = rows_st[nb].limit[r] == -INFINITY ? -INFINITY : rows_st[nb].ref[r];
+                    red_l[warp][nb * 8 + 2 * t + r] = rows_st[nb].sum[r];
                 }
             }
         }
-        auto put = [&](int nb, float *dst) {                 // this warp's accumulators of 8 rows to dst [8][ROWF]
+        // this warp's accumulators of 8 rows to dst [8][ROWF], element d at place_of(d): so neither order meets a bank twice
+        auto place_of = [](int d) { return d ^ ((d >> 4 & 1) << 2); };
+        auto put = [&](int nb, float *dst) {
+            if (order4) {                                    // a lane has D / 8 consecutive d of rows 2t, 2t + 1
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                const int d0 = order4 ? (D / 8) * g + 2 * mb : 16 * mb + g, d1 = order4 ? d0 + 1 : d0 + 8;
-                dst[(2 * t) * F::ROWF + d0] = O[nb][mb][0];
-                dst[(2 * t + 1) * F::ROWF + d0] = O[nb][mb][1];
-                dst[(2 * t) * F::ROWF + d1] = O[nb][mb][2];
-                dst[(2 * t + 1) * F::ROWF + d1] = O[nb][mb][3];
+                for (int mb = 0; mb < MB; mb += 2)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        *reinterpret_cast<float4 *>(dst + (2 * t + r) * F::ROWF + place_of((D / 8) * g + 2 * mb)) =
+                            make_float4(O[nb][mb][r], O[nb][mb][2 + r], O[nb][mb + 1][r], O[nb][mb + 1][2 + r]);
+            } else {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dst[(2 * t + (e & 1)) * F::ROWF + place_of(16 * mb + 8 * (e >> 1) + g)] = O[nb][mb][e];
             }
         };
         // element (row, d0 .. d0 + 3) over the warps w0 .. w0 + n - 1, whose accumulators lie `step` floats apart from src on
@@ -771,7 +826,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
 #pragma unroll 4
             for (int w = 0; w < n; ++w) {
                 const float mw = red_m[w0 + w][row], f = mw == -INFINITY ? 0.f : ex2(mw - M);
-                const float4 a = *reinterpret_cast<const float4 *>(src + w * step + (row & 7) * F::ROWF + d0);
+                const float4 a = *reinterpret_cast<const float4 *>(src + w * step + (row & 7) * F::ROWF + place_of(d0));
                 L += f * red_l[w0 + w][row];
                 acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
             }
