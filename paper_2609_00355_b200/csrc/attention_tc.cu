@@ -35,9 +35,11 @@
 // kWindow: a tile's pages are the entries of a list (packed.cuh), so a tile's halves need not be neighbours; a row sees the
 //   keys below `sinks`, those from its window's start on, and what is left of its ancestor set.  Rows of V that no row of
 //   the tile sees (a page's rest before the window, behind the sinks or behind the last key) are zeroed by a helper warp.
-// kHeld: pages below held_len come from the 4-bit pool.  One bulk copy brings a page's K or V codes into a ring of
-//   three raw tiles, four helper warps convert them (exactly) to bf16 in the operand tile, next to the halves that the tensor
-//   copies bring, so everything after that is the same.  An operand tile is then full when the copies and all four warps are.
+// kHeld: pages below held_len come from the 4-bit pool.  Four helper warps load a tile's codes into registers as soon as they
+//   have converted the tile before (exactly, to bf16, into the operand tile next to the halves that the tensor copies bring),
+//   so everything after that is the same.  An operand tile is full when the copies and all four warps are.  A ring of raw
+//   tiles filled by bulk copies was slower: what the producer thread does for a tile costs it 1.6 us beside the softmax
+//   warps (64 rows over 8704 positions 49 us).
 #include "kernels.cuh"
 #include "packed.cuh"
 #include "tc_ptx.cuh"
@@ -66,7 +68,6 @@ constexpr int ECG = NG;                  // column groups of the epilogue: a row
 enum { kWhole = 0, kWindow = 1, kHeld = 2 };                 // CACHE
 constexpr int n_helpers(int cache) { return cache == kHeld ? 4 : cache == kWindow ? 1 : 0; }       // warps behind the softmax warps
 constexpr int n_threads(int cache) { return 64 + NSOFT + 32 * n_helpers(cache); }
-constexpr int RAW = 3;                   // raw 4-bit tiles (K or V of 128 keys) in flight
 static_assert(CK == 32, "the visibility bit set of 32 keys is one word");
 
 // 16 accumulator columns of a row, combined over the softmax groups: sum_g w[g] * O_g.  Warp-collective.  Only the
@@ -105,19 +106,13 @@ struct Smem {
     // d 64 would fit twice into an SM's shared memory, and clusters whose CTAs hold the columns crosswise would wait for each
     // other in a cluster barrier
     static constexpr int TOTAL = OPER_BYTES + 1024 > (int)least_smem(TMEM_COLS) ? OPER_BYTES + 1024 : (int)least_smem(TMEM_COLS);
-    static constexpr int RAW_BYTES = 2 * packed::Tile<D>::HALF;          // K or V of two pages
-    static constexpr int total(int cache) {
-        const int need = OPER_BYTES + 1024 + (cache == kHeld ? RAW * RAW_BYTES : 0);
-        return need > TOTAL ? need : TOTAL;
-    }
     static_assert(O_COL + NG * D <= TMEM_COLS, "tensor memory budget");
     static_assert(RECV_AT + RECV_BYTES <= OPER_BYTES, "the merge fits the operand buffers");
     static_assert(RECV_AT % 16 == 0 && ROWF % 4 == 0, "bulk copies start on 16-byte boundaries");
 };
 
 struct alignas(8) AttnBars {
-    uint64_t q_ready, k_full[NG], k_empty[NG], v_full[NG], v_empty[NG], s_full[NG], p_full[NG], all_done, v_zero, merge;
-    uint64_t raw_full[RAW], raw_empty[RAW];              // kHeld
+    uint64_t q_ready, k_full[NG], k_empty[NG], v_full[NG], v_empty[NG], s_full[NG], p_full[NG], all_done, v_zero[NG], merge;
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -131,7 +126,6 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
     unsigned char *sQ = smem;                                        // hi plane, lo plane
     unsigned char *sK = sQ + Smem<D>::Q_BYTES;                       // tiles [slab][128 keys][128 bytes], one per group
     unsigned char *sV = sK + NG * KV_BYTES;
-    unsigned char *sRaw = sV + NG * KV_BYTES;                        // kHeld: raw tiles
     __shared__ AttnBars bars;
     __shared__ float red_m[NG][QT], red_l[NG][QT];        // the groups' reference maxima and row sums
 
@@ -162,14 +156,8 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
             mbar_init(&bars.p_full[b], 4);               // one arrival per warp of the group
         }
         mbar_init(&bars.all_done, 1);
-        mbar_init(&bars.v_zero, 1);
+        for (int b = 0; b < NG; ++b) mbar_init(&bars.v_zero[b], 1);
         mbar_init(&bars.merge, 1);
-        if constexpr (CACHE == kHeld) {
-            for (int b = 0; b < RAW; ++b) {
-                mbar_init(&bars.raw_full[b], 1);
-                mbar_init(&bars.raw_empty[b], 4);        // one arrival per helper warp
-            }
-        }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (p.S > 1) {
@@ -269,41 +257,8 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
             // K and V tiles advance independently, each as far ahead as its ring allows: one thread polls both rings
             uint64_t stall_t0 = 0;
             uint32_t spins = 0;
-            // kHeld: raw tiles in the order K, V of tile 0, K, V of tile 1, ..; a tile without held pages takes no slot
-            int raw_job = CACHE == kHeld ? 0 : 2 * nt, raw_used = 0;
-            while (issued_k < nt || issued_v < nt || raw_job < 2 * nt) {
+            while (issued_k < nt || issued_v < nt) {
                 bool progressed = false;
-                if constexpr (CACHE == kHeld) {
-                    if (raw_job < 2 * nt) {
-                        const int i = raw_job >> 1, kv = raw_job & 1, pages = min(2, np - 2 * i);
-                        int n = 0;
-                        for (int h = 0; h < pages; ++h) n += page_of(i, h) < held ? 1 : 0;
-                        const int slot = raw_used % RAW;
-                        if (n == 0) {
-                            ++raw_job;
-                            progressed = true;
-                        } else if (mbar_try_wait(&bars.raw_empty[slot], ((uint32_t)(raw_used / RAW) & 1u) ^ 1u)) {
-                            constexpr int HALF = packed::Tile<D>::HALF;
-                            mbar_expect_tx(&bars.raw_full[slot], (uint32_t)(n * HALF));
-                            for (int h = 0; h < pages; ++h) {
-                                const int pg = page_of(i, h);
-                                if (pg >= held) continue;
-                                int page = pg < p.geom.max_pages_per_seq ? p.held_table[(size_t)s * p.geom.max_pages_per_seq + pg] : -1;
-                                if (page < 0 || page >= p.held_pages) {
-                                    page = 0;
-                                    set_status(p.status, GLANCE_E_BOUNDS);
-                                }
-                                const unsigned char *src = p.held_layer + ((size_t)page * p.Hkv + kvh) * packed::Tile<D>::BYTES + kv * HALF;
-                                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                                             ::"r"(smem_u32(sRaw + slot * Smem<D>::RAW_BYTES + h * HALF)), "l"(src), "r"((uint32_t)HALF),
-                                               "r"(smem_u32(&bars.raw_full[slot])) : "memory");
-                            }
-                            ++raw_used;
-                            ++raw_job;
-                            progressed = true;
-                        }
-                    }
-                }
                 const int ks = issued_k & 1, vs = issued_v & 1;
                 if (issued_k < nt && mbar_try_wait(&bars.k_empty[ks], ((uint32_t)(issued_k >> 1) & 1u) ^ 1u)) {
                     load_tile(issued_k, 0, sK + ks * KV_BYTES, &bars.k_full[ks]);
@@ -330,14 +285,6 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                 }
             }
             if (!waited) pdl_wait();
-            if constexpr (CACHE == kHeld) {
-                if (*abort_flag)                         // raw copies already issued must land, too
-                    for (int i = max(0, raw_used - RAW); i < raw_used; ++i) {
-                        const uint64_t t0 = global_ns();
-                        while (!mbar_try_wait(&bars.raw_full[i % RAW], (uint32_t)(i / RAW) & 1u))
-                            if (global_ns() - t0 > kWaitLimitNs) break;
-                    }
-            }
         }
         // The page that holds the last key may continue with rows that belong to nobody (any bits, NaN included):
         // this warp zeroes them in the V tile once it has landed, and tells the MMA issuer.  The wait is exact:
@@ -357,7 +304,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.v_zero);
+                if (lane == 0) mbar_arrive(&bars.v_zero[0]);
             }
         }
         if (lane == 0) {
@@ -384,7 +331,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
             const int planes = p.q_lo ? 2 : 1;
             auto pages_of = [&](int i) { return min(2, np - 2 * i); };
             auto in_context = [&](int i) { return (CACHE ? (page_of(i, pages_of(i) - 1) + 1) : pg_begin + 2 * i + pages_of(i)) * kPage <= P; };
-            int zeroed = 0;                              // CACHE: tiles that waited for a helper's zeros
+            uint32_t zeroed = 0;                         // CACHE: bit b: parity of the waits for a helper's zeros in slot b so far
             auto issue_s = [&](int i) -> bool {
                 const int b = i & 1;
                 const int planes_i = (skip_q_lo && in_context(i)) ? 1 : planes;
@@ -415,10 +362,11 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                 // the rows after the last key have been zeroed by the producer warp
                 if constexpr (CACHE != kWhole) {
                     if (needs_zeros(i)) {
-                        if (!mbar_wait(&bars.v_zero, (uint32_t)zeroed & 1u, abort_flag, p.status)) { ok = false; break; }
-                        ++zeroed;
+                        // (a barrier a slot: the helper may be a tile ahead, but not two of the same slot)
+                        if (!mbar_wait(&bars.v_zero[b], zeroed >> b & 1u, abort_flag, p.status)) { ok = false; break; }
+                        zeroed ^= 1u << b;
                     }
-                } else if (i == nt - 1 && n_keys < pg_end * kPage && !mbar_wait(&bars.v_zero, 0, abort_flag, p.status)) { ok = false; break; }
+                } else if (i == nt - 1 && n_keys < pg_end * kPage && !mbar_wait(&bars.v_zero[0], 0, abort_flag, p.status)) { ok = false; break; }
                 if (!mbar_wait(&bars.p_full[b], ph, abort_flag, p.status)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t vbase = smem_u32(sV + b * KV_BYTES);
@@ -441,67 +389,107 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
     } else if (CACHE != kWhole && warp >= 2 + NSOFT / 32) {
         // ---------------- helper warps: 4-bit tiles -> bf16 operand tiles, zeros in rows of V that nobody sees ----------------
         const int helper = warp - 2 - NSOFT / 32;
-        int raw_used = 0;
         bool ok = true;
+        // kHeld: a thread converts groups of 16 (8 bytes of codes and a scale -> two 16-byte pieces of the key's row) of keys KEYS
+        // apart.  Eight lanes that store together meet no bank twice: the two slabs of a row lie on the same banks, so half of
+        // them take the neighbouring row's other slab.
+        constexpr int HALF = packed::Tile<D>::HALF, GROUPS = packed::Tile<D>::GROUPS, KEYS = 128 / GROUPS, PER = kPage / KEYS;
+        const int lc = lane % GROUPS;
+        const int lkey = helper * (32 / GROUPS) + (D == 128 ? 2 * (lane >> 4) + (((lane >> 3) ^ (lane >> 2)) & 1) : lane / GROUPS);
+        const uint32_t src_code = packed::code_at<D>(lkey, lc >> 1) + (lc & 1) * 8, src_scale = packed::Tile<D>::SCALES + lkey * GROUPS + lc;
+        uint32_t dst_piece[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int ch = 2 * lc + k;
+            dst_piece[k] = (uint32_t)((ch >> 3) * SLAB + lkey * 128 + (((ch & 7) ^ (lkey & 7)) << 4));
+        }
+        struct Codes {
+            uint2 w[2][PER];
+            uint32_t scale[2][PER];
+        };
+        // entries 32 at a time: a lane's page number, or -1 where the page is not held in 4 bits
+        auto look_up = [&](int v) {
+            const int pg = v < np ? list.page(pg_begin + v) : held;
+            if (pg >= held) return -1;
+            int page = pg < p.geom.max_pages_per_seq ? p.held_table[(size_t)s * p.geom.max_pages_per_seq + pg] : -1;
+            if (page < 0 || page >= p.held_pages) {
+                page = 0;
+                set_status(p.status, GLANCE_E_BOUNDS);
+            }
+            return page;
+        };
+        int numbers = -1, ahead = -1;
+        if constexpr (CACHE == kHeld) {
+            numbers = look_up(lane);
+            ahead = look_up(32 + lane);
+        }
+        // K (kv 0) or V of tile i into registers; `numbers` holds its pages
+        auto fetch = [&](int i, int kv, Codes &c) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int page = __shfl_sync(0xffffffffu, numbers, (2 * i + h) & 31);
+                if (page < 0) continue;
+                const unsigned char *tile = p.held_layer + ((size_t)page * p.Hkv + kvh) * packed::Tile<D>::BYTES + kv * HALF;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    c.w[h][j] = *reinterpret_cast<const uint2 *>(tile + src_code + j * KEYS * packed::Tile<D>::ROW);
+                    c.scale[h][j] = tile[src_scale + j * KEYS * GROUPS];
+                }
+            }
+        };
+        auto convert = [&](const Codes &c, bool h0, bool h1, uint32_t dst) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!(h ? h1 : h0)) continue;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const uint32_t s2 = packed::scales_to_half(c.scale[h][j] * 0x101u);
+                    uint32_t v[2][4];
+                    packed::codes_to_half(c.w[h][j].x, v[0]);
+                    packed::codes_to_half(c.w[h][j].y, v[1]);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k >> 2][k & 3] = packed::half2_to_bf16(packed::mul_half2(v[k >> 2][k & 3], s2));
+                    const uint32_t to = dst + (uint32_t)((h * kPage + j * KEYS) * 128);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + dst_piece[k]), "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
+                }
+            }
+            fence_async_smem();
+            __syncwarp();
+        };
+        Codes ck, cv;
+        if constexpr (CACHE == kHeld) {
+            if (nt > 0) {
+                fetch(0, 0, ck);
+                fetch(0, 1, cv);
+            }
+        }
         for (int i = 0; i < nt && ok; ++i) {
             const int b = i & 1, pages = min(2, np - 2 * i);
             const uint32_t ph = (uint32_t)(i >> 1) & 1u;
-            if constexpr (CACHE == kWindow) {
-                // every phase of the slot is seen, so that the wait for a tile below cannot take an older one for it
+            // every phase of a slot is seen, so that a wait for a tile cannot take an older one for it
+            if constexpr (CACHE == kHeld) {
+                const bool h0 = page_of(i, 0) < held, h1 = pages > 1 && page_of(i, 1) < held;
+                ok = mbar_wait(&bars.k_empty[b], ph ^ 1u, abort_flag, p.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                convert(ck, h0, h1, smem_u32(sK + b * KV_BYTES));
+                if (lane == 0) mbar_arrive(&bars.k_full[b]);
+                if ((i + 1) % 16 == 0) {
+                    numbers = ahead;
+                    ahead = look_up(2 * i + 2 + 32 + lane);
+                }
+                if (i + 1 < nt) fetch(i + 1, 0, ck);
                 ok = mbar_wait(&bars.v_empty[b], ph ^ 1u, abort_flag, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-            }
-            if constexpr (CACHE == kHeld) {
-                constexpr int HALF = packed::Tile<D>::HALF, GROUPS = packed::Tile<D>::GROUPS;
-                for (int kv = 0; kv < 2 && ok; ++kv) {
-                    const bool h0 = page_of(i, 0) < held, h1 = pages > 1 && page_of(i, 1) < held;
-                    uint64_t *full = kv ? &bars.v_full[b] : &bars.k_full[b];
-                    if (h0 || h1) {
-                        const int slot = raw_used % RAW;
-                        ok = mbar_wait(kv ? &bars.v_empty[b] : &bars.k_empty[b], ph ^ 1u, abort_flag, p.status) &&
-                             mbar_wait(&bars.raw_full[slot], (uint32_t)(raw_used / RAW) & 1u, abort_flag, p.status);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (!ok) break;
-                        const unsigned char *raw = sRaw + slot * Smem<D>::RAW_BYTES;
-                        unsigned char *dst = (kv ? sV : sK) + b * KV_BYTES;
-                        // a thread converts one group of 16: 8 bytes of codes and a scale -> two 16-byte pieces of the key's row
-#pragma unroll 2
-                        for (int it = helper * 32 + lane; it < 2 * kPage * GROUPS; it += 128) {
-                            const int h = it / (kPage * GROUPS), key = it / GROUPS % kPage, c = it % GROUPS;
-                            if (!(h ? h1 : h0)) continue;
-                            const uint2 w = *reinterpret_cast<const uint2 *>(raw + h * HALF + packed::code_at<D>(key, c >> 1) + (c & 1) * 8);
-                            const uint32_t sc = raw[h * HALF + packed::Tile<D>::SCALES + key * GROUPS + c];
-                            const uint32_t s2 = packed::scales_to_half(sc | sc << 8);
-                            uint32_t v[2][4];
-                            packed::codes_to_half(w.x, v[0]);
-                            packed::codes_to_half(w.y, v[1]);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                v[0][k] = packed::half2_to_bf16(packed::mul_half2(v[0][k], s2));
-                                v[1][k] = packed::half2_to_bf16(packed::mul_half2(v[1][k], s2));
-                            }
-                            const int row = h * kPage + key;
-                            // lanes of the first slab store their first piece while the second slab's store their second: no bank twice
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const int second = SLABS > 1 ? k ^ (c >> 2) : k, ch = 2 * c + second;
-                                const uint4 o = second ? make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]) : make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
-                                *reinterpret_cast<uint4 *>(dst + (ch >> 3) * SLAB + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = o;
-                            }
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bars.raw_empty[slot]);
-                        ++raw_used;
-                    } else {
-                        // nothing to convert: the arrival must not run ahead of the slot's previous tile
-                        ok = mbar_wait(kv ? &bars.v_empty[b] : &bars.k_empty[b], ph ^ 1u, abort_flag, p.status);
-                        ok = __all_sync(0xffffffffu, ok);
-                        if (!ok) break;
-                    }
-                    if (lane == 0) mbar_arrive(full);
-                }
+                convert(cv, h0, h1, smem_u32(sV + b * KV_BYTES));
+                if (lane == 0) mbar_arrive(&bars.v_full[b]);
+                if (i + 1 < nt) fetch(i + 1, 1, cv);
+            } else {
+                ok = mbar_wait(&bars.v_empty[b], ph ^ 1u, abort_flag, p.status);
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
             }
             if (helper == 0 && needs_zeros(i)) {
@@ -520,7 +508,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.v_zero);
+                if (lane == 0) mbar_arrive(&bars.v_zero[b]);
             }
         }
         __syncwarp();
@@ -902,14 +890,14 @@ template <int D, int CACHE>
 cudaError_t launch_d(const AttnParams &p, const CUtensorMap &map_kv, dim3 grid, cudaStream_t st) {
     static bool once = false;
     if (!once) {
-        cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, CACHE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::total(CACHE));
+        cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, CACHE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
         if (e != cudaSuccess) return e;
         once = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(n_threads(CACHE), 1, 1);
-    cfg.dynamicSmemBytes = Smem<D>::total(CACHE);
+    cfg.dynamicSmemBytes = Smem<D>::TOTAL;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -311,3 +311,12 @@ def test_packed_window(heads, held, kind, T, lens, window, sinks):
                                                       ("chain", 200, [700], 300, 64)])
 def test_two_terms(heads, held, kind, T, lens, window, sinks):
     run_attention(Cache(heads, lens, T, 14, held=held), kind, window, sinks, 6, two=True)
+
+
+@pytest.mark.gpu
+def test_zeroed_tiles_side_by_side():
+    """The sinks' end and the window's start in neighbouring tiles: rows that nobody sees are cleared in both, and the second may be
+    cleared before the first is used."""
+    for _ in range(20):
+        run_attention(Cache(H7, [2000, 500], 80, 13, held=100), "tree", 450, 200, 5)
+        run_attention(Cache(H7, [2000, 500], 80, 13), "tree", 450, 200, 5)
