@@ -35,9 +35,9 @@
 // kWindow: a tile's pages are the entries of a list (packed.cuh), so a tile's halves need not be neighbours; a row sees the
 //   keys below `sinks`, those from its window's start on, and what is left of its ancestor set.  Rows of V that no row of
 //   the tile sees (a page's rest before the window, behind the sinks or behind the last key) are zeroed by a helper warp.
-// kHeld: pages below held_len come from the 4-bit pool.  Four helper warps load a tile's codes into registers as soon as they
+// kHeld: pages below held_len come from the 4-bit pool.  Helper warps load a tile's codes into registers as soon as they
 //   have converted the tile before (exactly, to bf16, into the operand tile next to the halves that the tensor copies bring),
-//   so everything after that is the same.  An operand tile is full when the copies and all four warps are.  A ring of raw
+//   so everything after that is the same.  An operand tile is full when the copies and its warps are.  A ring of raw
 //   tiles filled by bulk copies was slower: what the producer thread does for a tile costs it 1.6 us beside the softmax
 //   warps (64 rows over 8704 positions 49 us).
 #include "kernels.cuh"
@@ -66,7 +66,8 @@ constexpr int P_TERMS = 2;               // bf16 terms of a probability
 constexpr int NSOFT = 128 * NG;          // softmax / epilogue threads: one per row and group
 constexpr int ECG = NG;                  // column groups of the epilogue: a row's d outputs are split over them
 enum { kWhole = 0, kWindow = 1, kHeld = 2 };                 // CACHE
-constexpr int n_helpers(int cache) { return cache == kHeld ? 4 : cache == kWindow ? 1 : 0; }       // warps behind the softmax warps
+constexpr int KV_HELPERS = 3;            // kHeld: warps that convert K, and as many for V
+__host__ __device__ constexpr int n_helpers(int cache) { return cache == kHeld ? 2 * KV_HELPERS : cache == kWindow ? 1 : 0; }       // warps behind the softmax warps
 constexpr int n_threads(int cache) { return 64 + NSOFT + 32 * n_helpers(cache); }
 static_assert(CK == 32, "the visibility bit set of 32 keys is one word");
 
@@ -148,9 +149,9 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
     if (threadIdx.x == 0) {
         mbar_init(&bars.q_ready, NSOFT / 32);            // one arrival per softmax warp
         for (int b = 0; b < NG; ++b) {
-            mbar_init(&bars.k_full[b], CACHE == kHeld ? 5 : 1);       // the copies, and one arrival per helper warp
+            mbar_init(&bars.k_full[b], CACHE == kHeld ? 1 + KV_HELPERS : 1);       // the copies, and one arrival per helper warp
             mbar_init(&bars.k_empty[b], 1);
-            mbar_init(&bars.v_full[b], CACHE == kHeld ? 5 : 1);
+            mbar_init(&bars.v_full[b], CACHE == kHeld ? 1 + KV_HELPERS : 1);
             mbar_init(&bars.v_empty[b], 1);
             mbar_init(&bars.s_full[b], 1);
             mbar_init(&bars.p_full[b], 4);               // one arrival per warp of the group
@@ -390,22 +391,17 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         // ---------------- helper warps: 4-bit tiles -> bf16 operand tiles, zeros in rows of V that nobody sees ----------------
         const int helper = warp - 2 - NSOFT / 32;
         bool ok = true;
-        // kHeld: a thread converts groups of 16 (8 bytes of codes and a scale -> two 16-byte pieces of the key's row) of keys KEYS
-        // apart.  Eight lanes that store together meet no bank twice: the two slabs of a row lie on the same banks, so half of
-        // them take the neighbouring row's other slab.
-        constexpr int HALF = packed::Tile<D>::HALF, GROUPS = packed::Tile<D>::GROUPS, KEYS = 128 / GROUPS, PER = kPage / KEYS;
+        // kHeld: warps 0..2 convert K, 3..5 V.  A lane converts groups of 16 (8 bytes of codes and a scale -> two 16-byte pieces of
+        // the key's row), a warp KEYS keys at a time, every third such step of a tile.  Eight lanes that store together meet no
+        // bank twice: the two slabs of a row lie on the same banks, so half of them take the neighbouring row's other slab.
+        const int kv = helper / KV_HELPERS, first = helper % KV_HELPERS;
+        constexpr int HALF = packed::Tile<D>::HALF, GROUPS = packed::Tile<D>::GROUPS, KEYS = 32 / GROUPS, STEPS = kPage / KEYS;      // of a page
+        constexpr int PER = (2 * STEPS + KV_HELPERS - 1) / KV_HELPERS;
         const int lc = lane % GROUPS;
-        const int lkey = helper * (32 / GROUPS) + (D == 128 ? 2 * (lane >> 4) + (((lane >> 3) ^ (lane >> 2)) & 1) : lane / GROUPS);
-        const uint32_t src_code = packed::code_at<D>(lkey, lc >> 1) + (lc & 1) * 8, src_scale = packed::Tile<D>::SCALES + lkey * GROUPS + lc;
-        uint32_t dst_piece[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int ch = 2 * lc + k;
-            dst_piece[k] = (uint32_t)((ch >> 3) * SLAB + lkey * 128 + (((ch & 7) ^ (lkey & 7)) << 4));
-        }
+        const int lkey = D == 128 ? 2 * (lane >> 4) + (((lane >> 3) ^ (lane >> 2)) & 1) : lane / GROUPS;      // within a step's keys
         struct Codes {
-            uint2 w[2][PER];
-            uint32_t scale[2][PER];
+            uint2 w[PER];
+            uint32_t scale[PER];
         };
         // entries 32 at a time: a lane's page number, or -1 where the page is not held in 4 bits
         auto look_up = [&](int v) {
@@ -423,76 +419,64 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
             numbers = look_up(lane);
             ahead = look_up(32 + lane);
         }
-        // K (kv 0) or V of tile i into registers; `numbers` holds its pages
-        auto fetch = [&](int i, int kv, Codes &c) {
+        // this warp's steps of K or V of tile i into registers; `numbers` holds its pages
+        auto fetch = [&](int i, Codes &c) {
+            const int page0 = __shfl_sync(0xffffffffu, numbers, 2 * i & 31), page1 = __shfl_sync(0xffffffffu, numbers, 2 * i + 1 & 31);
+            const unsigned char *tile0 = p.held_layer + ((size_t)max(page0, 0) * p.Hkv + kvh) * packed::Tile<D>::BYTES + kv * HALF;
+            const unsigned char *tile1 = p.held_layer + ((size_t)max(page1, 0) * p.Hkv + kvh) * packed::Tile<D>::BYTES + kv * HALF;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int page = __shfl_sync(0xffffffffu, numbers, (2 * i + h) & 31);
-                if (page < 0) continue;
-                const unsigned char *tile = p.held_layer + ((size_t)page * p.Hkv + kvh) * packed::Tile<D>::BYTES + kv * HALF;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    c.w[h][j] = *reinterpret_cast<const uint2 *>(tile + src_code + j * KEYS * packed::Tile<D>::ROW);
-                    c.scale[h][j] = tile[src_scale + j * KEYS * GROUPS];
-                }
+            for (int j = 0; j < PER; ++j) {
+                const int step = first + j * KV_HELPERS, h = step >= STEPS, key = (step - h * STEPS) * KEYS + lkey;
+                if (step >= 2 * STEPS || (h ? page1 : page0) < 0) continue;
+                const unsigned char *tile = h ? tile1 : tile0;
+                c.w[j] = *reinterpret_cast<const uint2 *>(tile + packed::code_at<D>(key, lc >> 1) + (lc & 1) * 8);
+                c.scale[j] = tile[packed::Tile<D>::SCALES + key * GROUPS + lc];
             }
         };
         auto convert = [&](const Codes &c, bool h0, bool h1, uint32_t dst) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (!(h ? h1 : h0)) continue;
+            for (int j = 0; j < PER; ++j) {
+                const int step = first + j * KV_HELPERS, h = step >= STEPS, row = step * KEYS + lkey;
+                if (step >= 2 * STEPS || !(h ? h1 : h0)) continue;
+                const uint32_t s2 = packed::scales_to_half(c.scale[j] * 0x101u);
+                uint32_t v[2][4];
+                packed::codes_to_half(c.w[j].x, v[0]);
+                packed::codes_to_half(c.w[j].y, v[1]);
 #pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const uint32_t s2 = packed::scales_to_half(c.scale[h][j] * 0x101u);
-                    uint32_t v[2][4];
-                    packed::codes_to_half(c.w[h][j].x, v[0]);
-                    packed::codes_to_half(c.w[h][j].y, v[1]);
+                for (int k = 0; k < 8; ++k) v[k >> 2][k & 3] = packed::half2_to_bf16(packed::mul_half2(v[k >> 2][k & 3], s2));
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k >> 2][k & 3] = packed::half2_to_bf16(packed::mul_half2(v[k >> 2][k & 3], s2));
-                    const uint32_t to = dst + (uint32_t)((h * kPage + j * KEYS) * 128);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + dst_piece[k]), "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
+                for (int k = 0; k < 2; ++k) {
+                    const int ch = 2 * lc + k;
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + (uint32_t)((ch >> 3) * SLAB + row * 128 + (((ch & 7) ^ (row & 7)) << 4))),
+                                 "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
                 }
             }
             fence_async_smem();
             __syncwarp();
         };
-        Codes ck, cv;
+        Codes codes;
         if constexpr (CACHE == kHeld) {
-            if (nt > 0) {
-                fetch(0, 0, ck);
-                fetch(0, 1, cv);
-            }
+            if (nt > 0) fetch(0, codes);
         }
+        uint64_t *const empty = kv ? bars.v_empty : bars.k_empty, *const full = kv ? bars.v_full : bars.k_full;
         for (int i = 0; i < nt && ok; ++i) {
             const int b = i & 1, pages = min(2, np - 2 * i);
             const uint32_t ph = (uint32_t)(i >> 1) & 1u;
             // every phase of a slot is seen, so that a wait for a tile cannot take an older one for it
+            ok = mbar_wait(CACHE == kHeld ? &empty[b] : &bars.v_empty[b], ph ^ 1u, abort_flag, p.status);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
             if constexpr (CACHE == kHeld) {
-                const bool h0 = page_of(i, 0) < held, h1 = pages > 1 && page_of(i, 1) < held;
-                ok = mbar_wait(&bars.k_empty[b], ph ^ 1u, abort_flag, p.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                convert(ck, h0, h1, smem_u32(sK + b * KV_BYTES));
-                if (lane == 0) mbar_arrive(&bars.k_full[b]);
+                convert(codes, page_of(i, 0) < held, pages > 1 && page_of(i, 1) < held, smem_u32((kv ? sV : sK) + b * KV_BYTES));
+                if (lane == 0) mbar_arrive(&full[b]);
                 if ((i + 1) % 16 == 0) {
                     numbers = ahead;
                     ahead = look_up(2 * i + 2 + 32 + lane);
                 }
-                if (i + 1 < nt) fetch(i + 1, 0, ck);
-                ok = mbar_wait(&bars.v_empty[b], ph ^ 1u, abort_flag, p.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                convert(cv, h0, h1, smem_u32(sV + b * KV_BYTES));
-                if (lane == 0) mbar_arrive(&bars.v_full[b]);
-                if (i + 1 < nt) fetch(i + 1, 1, cv);
-            } else {
-                ok = mbar_wait(&bars.v_empty[b], ph ^ 1u, abort_flag, p.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+                if (i + 1 < nt) fetch(i + 1, codes);
             }
-            if (helper == 0 && needs_zeros(i)) {
+            constexpr int CLEARER = n_helpers(CACHE) - 1;
+            if (helper == CLEARER && needs_zeros(i)) {
                 // the tile has landed; its second MMA waits for this warp
                 ok = mbar_wait(&bars.v_full[b], ph, abort_flag, p.status);
                 ok = __all_sync(0xffffffffu, ok);
