@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         kvh = i % p.Hkv;
     }
     const int s = blockIdx.z / p.S, split = blockIdx.z % p.S;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;     // (a uniform value to the compiler)
 
     if (threadIdx.x == 0) {
         mbar_init(&bars.q_ready, NSOFT / 32);            // one arrival per softmax warp
@@ -327,7 +327,10 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         // ---------------- MMA issuer ----------------
         // The scores of the first two tiles are issued up front; after P V of tile i the scores of tile i + 2 follow into
         // the buffer that P V has just read (MMAs of one thread execute in order).
-        if (lane == 0 && nt > 0) {
+        // The whole warp walks the loop and one lane issues: descriptors then stay in uniform registers, where the instruction
+        // wants them.  With one lane in the loop an MMA took it 78 ns to issue for 34 of work.
+        if (nt > 0) {
+            const uint32_t lead = lane == 0 ? 1u : 0u;
             const uint32_t idesc_o = umma_idesc_bmn(D);           // M 128, N d, B = V is MN-major
             const int planes = p.q_lo ? 2 : 1;
             auto pages_of = [&](int i) { return min(2, np - 2 * i); };
@@ -346,12 +349,12 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks) {
                         const int sl = ks >> 2, kk = ks & 3;
-                        umma_f16(tmem_S + (uint32_t)(b * KT), umma_desc(qbase + sl * QT * 128) + (uint64_t)(kk * 2),
+                        umma_f16_by(lead, tmem_S + (uint32_t)(b * KT), umma_desc(qbase + sl * QT * 128) + (uint64_t)(kk * 2),
                                  umma_desc(kbase + sl * SLAB) + (uint64_t)(kk * 2), idesc_s, (pl | ks) > 0 ? 1u : 0u);
                     }
                 }
-                umma_commit(&bars.k_empty[b]);            // K tile free once these MMAs have read it
-                umma_commit(&bars.s_full[b]);
+                umma_commit_by(lead, &bars.k_empty[b]);            // K tile free once these MMAs have read it
+                umma_commit_by(lead, &bars.s_full[b]);
                 return true;
             };
             bool ok = mbar_wait(&bars.q_ready, 0, abort_flag, p.status);
@@ -379,12 +382,12 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
 #pragma unroll
                     for (int kk = 0; kk < 2; ++kk)
                         for (int pt = 0; pt < p_terms; ++pt)
-                            umma_f16_ts(tmem_O + (uint32_t)(b * D), tmem_S + (uint32_t)(b * KT + c * CK + pt * (CK / 2) + kk * 8),
+                            umma_f16_ts_by(lead, tmem_O + (uint32_t)(b * D), tmem_S + (uint32_t)(b * KT + c * CK + pt * (CK / 2) + kk * 8),
                                         umma_desc_mn(vbase + (c * CK + kk * 16) * 128, SLAB), idesc_o, (i >= NG || (c | kk | pt) > 0) ? 1u : 0u);
-                umma_commit(&bars.v_empty[b]);            // V tile free once these MMAs have read it
+                umma_commit_by(lead, &bars.v_empty[b]);            // V tile free once these MMAs have read it
                 if (i + NG < nt && !issue_s(i + NG)) { ok = false; break; }
             }
-            if (ok) umma_commit(&bars.all_done);         // every MMA of this CTA has completed when this barrier flips
+            if (ok) umma_commit_by(lead, &bars.all_done);         // every MMA of this CTA has completed when this barrier flips
         }
         __syncwarp();
     } else if (CACHE != kWhole && warp >= 2 + NSOFT / 32) {
