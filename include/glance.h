@@ -232,7 +232,8 @@ int32_t glance_set_packed(glance_ctx *ctx, const glance_packed *packed);
 
 /* Moves finished pages of every sequence and target layer from kv_pool into the registered 4-bit pool: len[s] rises to
  * max(0, seq_len[s] - keep) rounded down to whole pages (and never falls here).  keep >= 0 positions at least stay in bf16.
- * The bf16 pages are left as they are.  GLANCE_E_STATE without a registered pool. */
+ * The bf16 pages are left as they are.  kv_pool has to be 32-byte aligned here and in glance_unpack_cache.  GLANCE_E_STATE
+ * without a registered pool. */
 int32_t glance_pack_cache(glance_ctx *ctx, const glance_seqs *seqs, int32_t keep);
 
 /* The way back: len[s] falls to new_len[s] rounded down to whole pages (device [batch]; larger values change nothing), and

@@ -372,12 +372,13 @@ class Engine:
     def glance_unpack_cache(self, new_len: torch.Tensor, kv_pool: Optional[torch.Tensor] = None):
         """Pages from new_len [batch] (int32, device) on back to bf16: into the engine's pool, or into another of its shape."""
         assert new_len.dtype == torch.int32 and new_len.numel() == self.batch
-        seqs = self.seqs
         if kv_pool is not None:
             assert kv_pool.shape == self.kv_pool.shape and kv_pool.dtype == self.kv_pool.dtype
-            seqs = Seqs.from_buffer_copy(self.seqs)
-            seqs.kv_pool = _ptr(kv_pool)
-        _check(self.lib.glance_unpack_cache(self.ctx, C.byref(seqs), _ptr(new_len)), "glance_unpack_cache")
+            self.seqs.kv_pool = _ptr(kv_pool)
+        try:
+            _check(self.lib.glance_unpack_cache(self.ctx, C.byref(self.seqs), _ptr(new_len)), "glance_unpack_cache")
+        finally:
+            self.seqs.kv_pool = self.kv_pool.data_ptr()
 
     def glance_attention(self, layer: int, q: torch.Tensor, T: int, out: torch.Tensor, anc: Optional[torch.Tensor] = None,
                          causal: bool = False, window: int = 0, sinks: int = 0, q_lo: Optional[torch.Tensor] = None,

@@ -824,6 +824,8 @@ static int32_t pack_common(glance_ctx *ctx, const glance_seqs *seqs, int32_t kee
     const int32_t rc = check_seqs(ctx, seqs);
     if (rc) return rc;
     if (keep < 0) return GLANCE_E_INVALID_ARG;
+    if ((uintptr_t)seqs->kv_pool & 31) return GLANCE_E_INVALID_ARG;
+    if ((double)seqs->batch * ctx->cfg.max_pages_per_seq * ctx->cfg.n_layers * 2 * ctx->cfg.n_kv_heads > 2e9) return GLANCE_E_CAPACITY;
     if (!ctx->held.pool) return GLANCE_E_STATE;
     PackParams pp{};
     pp.batch = seqs->batch; pp.n_layers = ctx->cfg.n_layers; pp.keep = keep; pp.seq_len = seqs->seq_len; pp.new_len = new_len;

@@ -17,20 +17,23 @@ namespace {
 using namespace packed;
 
 constexpr int kPackThreads = 256;
+constexpr int kPackBlocks = 4;   // an SM
 constexpr int kMaxSeqs = 64;
 
 __device__ __forceinline__ int whole_pages(int n) { return max(n, 0) / kPage; }
 
-// e4m3 of a / 6 for a = max|x| >= 0: both roundings (the quotient's to fp32, its to e4m3) act as one, because a has eight
-// significant bits: a / 6 is either a border of e4m3 exactly or further from one than fp32 rounds.
+// e4m3 of a / 6 for a = max|x| >= 0.  a has eight significant bits, so a / 6 is a border of e4m3 exactly or at least 2^-9 of
+// itself away from one: rounding the product with 1 / 6 (off by 2^-23) to 12 bits makes borders exact again.
 __device__ __forceinline__ uint32_t scale_code(float a) {
+    const float q = fminf(a * (1.f / 6.f), 1024.f);      // (saturates at 448)
+    const float wide = __fmul_rn(q, 4097.f), twelve = __fsub_rn(wide, __fsub_rn(wide, q));
     uint32_t r;
-    asm("{\n\t.reg .b16 x;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %1, %2;\n\tcvt.u32.u16 %0, x;\n\t}" : "=r"(r) : "f"(0.f), "f"(__fdiv_rn(a, 6.f)));
+    asm("{\n\t.reg .b16 x;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %1, %2;\n\tcvt.u32.u16 %0, x;\n\t}" : "=r"(r) : "f"(0.f), "f"(twelve));
     return r & 0xffu;
 }
 // e2m1 of x / s for two values (a in the low nibble), r = 1 / s rounded.  A quotient of an eight-bit and a four-bit
 // significand is a border of e2m1 (an odd multiple of 1/4, 1/2 or 1) exactly or at least 2^-10 away from one.  So it may be
-// rounded to a multiple of 2^-13, which undoes the rounding of r (2^-20 at most where it matters) and keeps ties ties.
+// rounded to a multiple of 2^-13, which undoes the rounding of r (one place: 2^-19 at most where it matters) and keeps ties ties.
 __device__ __forceinline__ uint32_t value_codes(float a, float b, float r) {
     constexpr float kGrid = 1536.f;                      // 1.5 * 2^10: its last place is 2^-13
     const float qa = __fsub_rn(__fmaf_rn(a, r, kGrid), kGrid), qb = __fsub_rn(__fmaf_rn(b, r, kGrid), kGrid);
@@ -42,17 +45,29 @@ __device__ __forceinline__ uint32_t value_codes(float a, float b, float r) {
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// A group's 32 bytes of bf16 in one access: as two of 16 a warp's accesses would cover half of every sector each time.
+__device__ __forceinline__ void load32(const void *p, uint4 (&v)[2]) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store32(void *p, const uint4 (&v)[2]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "r"(v[0].x), "r"(v[0].y), "r"(v[0].z), "r"(v[0].w), "r"(v[1].x), "r"(v[1].y), "r"(v[1].z), "r"(v[1].w) : "memory");
+}
+
 // 16 bf16 values -> 8 bytes of codes and the scale's code
 __device__ __forceinline__ uint2 pack_group(const uint4 (&v)[2], uint32_t &scale) {
     const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
-    uint32_t top = 0;                                    // the largest magnitude, by its bits
+    uint32_t both = 0;                                   // the largest magnitude, by its bits
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+    for (int i = 0; i < 8; ++i) both = __vmaxu2(both, w[i] & 0x7fff7fffu);
+    const uint32_t top = max(both & 0xffffu, both >> 16);
     scale = top >= 0x7f80u ? 0x7fu : scale_code(__uint_as_float(top << 16));
     __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)scale, __NV_E4M3);
     const float s = __half2float(__half(h));
     const bool live = s > 0.f;                           // a scale of 0 or NaN: codes 0
-    const float r = __frcp_rn(s);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     uint2 out = make_uint2(0u, 0u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -76,7 +91,7 @@ __device__ __forceinline__ void unpack_group(uint2 c, uint32_t scale, uint4 (&v)
 }
 
 template <int D, bool BACK>
-__global__ void __launch_bounds__(kPackThreads) pack_kernel(PackParams p) {
+__global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(PackParams p) {
     constexpr int GROUPS = Tile<D>::GROUPS;
     __shared__ int sh_first[kMaxSeqs], sh_upto[kMaxSeqs + 1], sh_len[kMaxSeqs];      // first page due, pages due up to here, new length
     __shared__ int sh_last;
@@ -111,67 +126,82 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(PackParams p) {
     __syncthreads();
     if (sh_last && t < p.batch) p.len[t] = sh_len[t];
 
-    const int pages = sh_upto[p.batch];
-    const int H = p.geom.n_kv_heads;
-    const size_t layer4 = (size_t)p.n_pages4 * H * Tile<D>::BYTES;
-    // item: layer, page, head, K|V
-    const long long items = (long long)pages * p.n_layers * H * 2;
-    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-        const int kvh = (int)(it % (2 * H));
-        const long long rest = it / (2 * H);
-        const int pg = (int)(rest % pages), layer = (int)(rest / pages);
-        const int kv = kvh & 1, head = kvh >> 1;
+    const unsigned pages = (unsigned)sh_upto[p.batch], H2 = 2u * (unsigned)p.geom.n_kv_heads;
+    const size_t layer4 = (size_t)p.n_pages4 * p.geom.n_kv_heads * Tile<D>::BYTES;
+    // item: layer, page, (head, K|V)
+    const unsigned items = pages * H2 * (unsigned)p.n_layers;
+    constexpr int STEPS = kPage * GROUPS / kPackThreads;
+    static_assert(kPage * GROUPS % kPackThreads == 0, "whole steps");
+    struct Item {
+        bf16 *rows;              // nullptr: nothing to move
+        unsigned char *tile;
+    };
+    auto find = [&](unsigned it) {
+        Item r{nullptr, nullptr};
+        if (it >= items) return r;
+        const unsigned kvh = it % H2, rest = it / H2, pg = rest % pages, layer = rest / pages;
+        const int kv = (int)(kvh & 1u), head = (int)(kvh >> 1);
         int s = 0;
-        while (sh_upto[s + 1] <= pg) ++s;
-        const int page = sh_first[s] + pg - sh_upto[s];
-        const int from = p.page_table[(size_t)s * p.geom.max_pages_per_seq + page];
-        const int at4 = p.page_table4[(size_t)s * p.geom.max_pages_per_seq + page];
+        while ((unsigned)sh_upto[s + 1] <= pg) ++s;
+        const size_t entry = (size_t)s * p.geom.max_pages_per_seq + sh_first[s] + (int)pg - sh_upto[s];
+        const int from = p.page_table[entry], at4 = p.page_table4[entry];
         if (from < 0 || from >= p.geom.n_pages || at4 < 0 || at4 >= p.n_pages4) {
             if (t == 0) set_status(p.status, GLANCE_E_BOUNDS);
-            continue;
+            return r;
         }
-        bf16 *rows = p.kv_pool + (size_t)layer * p.geom.layer_stride() + p.geom.row(from, kv, head, 0);
-        unsigned char *tile = p.pool4 + layer * layer4 + ((size_t)at4 * H + head) * Tile<D>::BYTES + kv * Tile<D>::HALF;
-        constexpr int STEPS = kPage * GROUPS / kPackThreads;
-        static_assert(kPage * GROUPS % kPackThreads == 0, "whole steps");
-        if (!BACK) {
-            uint4 v[STEPS][2];
+        r.rows = p.kv_pool + (size_t)layer * p.geom.layer_stride() + p.geom.row(from, kv, head, 0);
+        r.tile = p.pool4 + layer * layer4 + ((size_t)at4 * p.geom.n_kv_heads + head) * Tile<D>::BYTES + kv * Tile<D>::HALF;
+        return r;
+    };
+    struct Data {
+        uint4 v[STEPS][BACK ? 1 : 2];                    // two pieces of a row, or (way back) 8 bytes of codes and the scale
+    };
+    auto load = [&](const Item &it, Data &d) {
+        if (!it.rows) return;
 #pragma unroll
-            for (int u = 0; u < STEPS; ++u) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(rows) + (size_t)(u * kPackThreads + t) * 2;
-                v[u][0] = __ldcs(src);
-                v[u][1] = __ldcs(src + 1);
+        for (int u = 0; u < STEPS; ++u) {
+            const int g = u * kPackThreads + t;
+            if constexpr (!BACK) {
+                load32(it.rows + (size_t)g * kGroup, d.v[u]);
+            } else {
+                const int key = g / GROUPS, c = g % GROUPS;
+                const uint2 codes = __ldcs(reinterpret_cast<const uint2 *>(it.tile + code_at<D>(key, c >> 1) + (c & 1) * 8));
+                d.v[u][0] = make_uint4(codes.x, codes.y, it.tile[Tile<D>::SCALES + g], 0u);
             }
+        }
+    };
+    // The next item's loads are issued, and the page numbers of the one after it looked up, before this one's are converted.
+    Data now;
+    Item item = find(blockIdx.x);
+    load(item, now);
+    Item following = find(blockIdx.x + gridDim.x);
+    for (unsigned it = blockIdx.x; it < items; it += gridDim.x) {
+        Data next;
+        load(following, next);
+        const Item after = find(it + 2 * gridDim.x);
+        if (item.rows) {
 #pragma unroll
             for (int u = 0; u < STEPS; ++u) {
                 const int g = u * kPackThreads + t, key = g / GROUPS, c = g % GROUPS;
-                uint32_t scale;
-                const uint2 codes = pack_group(v[u], scale);
-                *reinterpret_cast<uint2 *>(tile + code_at<D>(key, c >> 1) + (c & 1) * 8) = codes;
-                // four neighbours' scales in one store
-                uint32_t four = scale << (8 * (t & 3));
-                four |= __shfl_xor_sync(0xffffffffu, four, 1);
-                four |= __shfl_xor_sync(0xffffffffu, four, 2);
-                if ((t & 3) == 0) *reinterpret_cast<uint32_t *>(tile + Tile<D>::SCALES + g) = four;
-            }
-        } else {
-            uint2 codes[STEPS];
-            uint32_t scale[STEPS];
-#pragma unroll
-            for (int u = 0; u < STEPS; ++u) {
-                const int g = u * kPackThreads + t, key = g / GROUPS, c = g % GROUPS;
-                codes[u] = __ldcs(reinterpret_cast<const uint2 *>(tile + code_at<D>(key, c >> 1) + (c & 1) * 8));
-                scale[u] = tile[Tile<D>::SCALES + g];
-            }
-#pragma unroll
-            for (int u = 0; u < STEPS; ++u) {
-                uint4 v[2];
-                unpack_group(codes[u], scale[u], v);
-                uint4 *dst = reinterpret_cast<uint4 *>(rows) + (size_t)(u * kPackThreads + t) * 2;
-                dst[0] = v[0];
-                dst[1] = v[1];
+                if constexpr (!BACK) {
+                    uint32_t scale;
+                    const uint2 codes = pack_group(now.v[u], scale);
+                    *reinterpret_cast<uint2 *>(item.tile + code_at<D>(key, c >> 1) + (c & 1) * 8) = codes;
+                    // four neighbours' scales in one store
+                    uint32_t four = scale << (8 * (t & 3));
+                    four |= __shfl_xor_sync(0xffffffffu, four, 1);
+                    four |= __shfl_xor_sync(0xffffffffu, four, 2);
+                    if ((t & 3) == 0) *reinterpret_cast<uint32_t *>(item.tile + Tile<D>::SCALES + g) = four;
+                } else {
+                    uint4 v[2];
+                    unpack_group(make_uint2(now.v[u][0].x, now.v[u][0].y), now.v[u][0].z, v);
+                    store32(item.rows + (size_t)g * kGroup, v);
+                }
             }
         }
+        item = following;
+        following = after;
+        now = next;
     }
 }
 
@@ -180,7 +210,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(PackParams p) {
 void launch_pack(const PackParams &p, bool back, cudaStream_t st) {
     // one wave: every block has to be counted in before the lengths may change, and a block strides over the tiles
     const long long most = (long long)p.batch * p.geom.max_pages_per_seq * p.n_layers * p.geom.n_kv_heads * 2;
-    const int blocks = (int)(most < 148 * 8 ? most : 148 * 8);
+    const int blocks = (int)(most < 148 * kPackBlocks ? most : 148 * kPackBlocks);
     if (p.geom.head_dim == 128) {
         if (back) pack_kernel<128, true><<<blocks, kPackThreads, 0, st>>>(p);
         else pack_kernel<128, false><<<blocks, kPackThreads, 0, st>>>(p);
