@@ -320,3 +320,331 @@ def test_zeroed_tiles_side_by_side():
     for _ in range(20):
         run_attention(Cache(H7, [2000, 500], 80, 13, held=100), "tree", 450, 200, 5)
         run_attention(Cache(H7, [2000, 500], 80, 13), "tree", 450, 200, 5)
+
+
+# ---- the target's own passes ---------------------------------------------------------------------------------------
+def oracle_pass(sh, tw, K, V, x, pos, P, masks):
+    """The target over rows x at cache rows P.. with one visibility mask a layer (the oracle's layer, this file's masks)."""
+    from oracle import glance_oracle as O
+    rows = torch.arange(P, P + x.shape[0])
+    for l, lw in enumerate(tw["layers"]):
+        x = O.decoder_layer(sh, lw, x, pos, K[l], V[l], rows, masks[l])
+    return O.rmsnorm(x, tw["final_norm"], sh.rms_eps) @ tw["lm_head"].T, x
+
+
+def seeded_engine(cfg, lens, seed, held=None):
+    """An engine and the oracle's widened weights over the same random cache (and what the 4-bit part of it stands for)."""
+    from oracle import glance_oracle as O
+    from paper_2609_00355_b200.binding import Engine, PackedCache
+    tb, hb = synth.make_weights(cfg, "cpu", 0)
+    dev = lambda w: {k: ([{a: b.cuda() for a, b in x.items()} for x in v] if isinstance(v, list) else v.cuda()) for k, v in w.items()}
+    eng = Engine(cfg, dev(tb), dev(hb), batch=len(lens), max_len=max(lens) + 4 * cfg.tree_N + 256, stream=torch.cuda.Stream())
+    with torch.cuda.stream(eng.stream):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        eng.kv_pool.copy_(torch.randn(eng.kv_pool.shape, device="cuda", generator=g) * 0.5)
+        eng.head_kv_all.copy_(torch.randn(eng.head_kv_all.shape, device="cuda", generator=g) * 0.5)
+        eng.seq_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        eng.root.copy_(torch.randint(0, cfg.vocab, (len(lens),), generator=g, device="cuda", dtype=torch.int32))
+        cap = max(lens) + 2 * cfg.tree_N + 8
+        K = [[torch.zeros(cap, cfg.n_kv_heads, cfg.head_dim) for _ in range(cfg.n_layers)] for _ in lens]
+        V = [[torch.zeros(cap, cfg.n_kv_heads, cfg.head_dim) for _ in range(cfg.n_layers)] for _ in lens]
+        n4 = [0] * len(lens)
+        if held is not None:
+            eng.glance_set_packed(PackedCache(eng))
+            eng.glance_pack_cache(keep=held)
+            n4 = eng.packed.len.tolist()
+        for s, P in enumerate(lens):
+            for l in range(cfg.n_layers):
+                k, v = eng.gather_kv(s, l, P)
+                for dst, src in ((K[s][l], k), (V[s][l], v)):
+                    dst[:P] = src.float().cpu()
+                    dst[: n4[s]] = held_values(src[: n4[s]]).float().cpu()
+            for p in range(n4[s] // PAGE):
+                eng.kv_pool[:, int(eng.page_table[s, p])] = math.nan
+    torch.cuda.synchronize()
+    return eng, O.Shape.of(cfg), O.widen(tb), K, V
+
+
+def relative(got, ref):
+    return float((got.double().cpu() - ref.double()).abs().max()) / float(ref.abs().max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("held", [None, 70])
+@pytest.mark.parametrize("windows,sinks,N", [((0, 100), 4, 8), ((64, 0), 70, 32), ((30, 300), 0, 1), ((5, 5), 1, 24)])
+def test_verify_pass_with_windows_a_layer(windows, sinks, N, held):
+    """glance_set_window and glance_set_packed in a verify pass of two layers, ragged batch, against the oracle's layers (logits and
+    hidden rows within the 2e-2 of the parity tests); then without them, the same bits as an engine that never had them."""
+    from tests import parity_harness as H
+    from oracle import glance_oracle as O
+    cfg = synth.CONFIGS["tiny"].replace(tree_N=N, batch=2)
+    lens = [333, 130]
+    eng, sh, tw, K, V = seeded_engine(cfg, lens, 21, held)
+    with torch.cuda.stream(eng.stream):
+        eng.glance_set_window(windows, sinks)
+        rng = np.random.default_rng(4)
+        trees = []
+        for s, P in enumerate(lens):
+            parent = random_parents(N, rng)
+            for i in range(1, N):
+                parent[i] = max(parent[i], 0)             # one tree, no padding rows
+            depth = np.zeros(N, dtype=np.int32)
+            for i in range(1, N):
+                depth[i] = depth[parent[i]] + 1
+            trees.append(O.tree_from_arrays(rng.integers(0, cfg.vocab, N), parent, depth, N))
+        H.tree_to_device(eng, trees)
+        logits = torch.zeros(2, N, cfg.vocab, device="cuda")
+        eng.glance_verify_tree(logits_dbg=logits)
+        eng.check_device_status()
+        for s, P in enumerate(lens):
+            t = trees[s]
+            masks = [torch.from_numpy(visible(P, N, "tree", t.parent, w, sinks if w else 0)) for w in windows]
+            x = tw["embed"][torch.as_tensor(t.token, dtype=torch.long)].clone()
+            ref, hid = oracle_pass(sh, tw, K[s], V[s], x, torch.as_tensor(P + t.depth.astype(np.int64)), P, masks)
+            assert relative(logits[s], ref) <= 2e-2
+            assert relative(eng.hidden[s], hid) <= 2e-2
+    if held is None:
+        other, *_ = seeded_engine(cfg, lens, 21)
+        with torch.cuda.stream(eng.stream):
+            eng.glance_set_window(None)
+            eng.kv_pool.copy_(other.kv_pool)
+            eng.glance_verify_tree(logits_dbg=logits)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other.stream):
+            H.tree_to_device(other, trees)
+            plain = torch.zeros_like(logits)
+            other.glance_verify_tree(logits_dbg=plain)
+        torch.cuda.synchronize()
+        assert torch.equal(plain, logits)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prior,count,windows,sinks,held", [(0, 150, (40, 0), 3, None), (200, 77, (64, 100), 65, 0), (333, 130, (0, 50), 0, 100)])
+def test_prefill_with_windows(prior, count, windows, sinks, held):
+    """A prefill pass of the second sequence of a batch: the new K/V rows of the last layer come from windowed rows of the first."""
+    cfg = synth.CONFIGS["tiny"].replace(batch=2)
+    eng, sh, tw, K, V = seeded_engine(cfg, [64, prior], 22, held)
+    with torch.cuda.stream(eng.stream):
+        eng.glance_set_window(windows, sinks)
+        emb = torch.randn(count, cfg.hidden, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16)
+        eng.glance_prefill(1, embeds=emb.cuda())
+        eng.check_device_status()
+        masks = [torch.from_numpy(visible(prior, count, "chain", None, w, sinks if w else 0)) for w in windows]
+        oracle_k = [torch.cat([k, torch.zeros(count, *k.shape[1:])]) for k in K[1]]
+        oracle_v = [torch.cat([v, torch.zeros(count, *v.shape[1:])]) for v in V[1]]
+        oracle_pass(sh, tw, oracle_k, oracle_v, emb.float(), torch.arange(prior, prior + count), prior, masks)
+        for l in range(cfg.n_layers):
+            k, v = eng.gather_kv(1, l, prior + count)
+            assert relative(k[prior:].float(), oracle_k[l][prior : prior + count]) <= 2e-2
+            assert relative(v[prior:].float(), oracle_v[l][prior : prior + count]) <= 2e-2
+        assert eng.seq_len.tolist() == [64, prior + count]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,N", [("tiny", 8), ("tiny", 1), ("small", 32)])
+def test_rounds_over_a_packed_cache_replayed_as_a_graph(name, N):
+    """Draft, tree, verify, commit and packing as one graph, against the same calls one by one: the same bits, round after round,
+    while pages move from bf16 to 4 bits; the cache that is left is what the plain calls leave."""
+    from tests import parity_harness as H
+    cfg = synth.CONFIGS[name].replace(tree_N=N, batch=2, n_layers=2)
+    engs = [seeded_engine(cfg, [190, 127], 23, 64)[0] for _ in range(2)]
+    logs = [[], []]
+    for which, eng in enumerate(engs):
+        with torch.cuda.stream(eng.stream):
+            eng.glance_set_window((0, 90), 5)
+            logits = torch.zeros(2, N, cfg.vocab, device="cuda")
+
+            def step():
+                eng.glance_draft_block()
+                eng.glance_build_tree()
+                eng.glance_verify_tree(logits_dbg=logits)
+                eng.glance_accept_commit()
+                eng.glance_pack_cache(keep=64)
+            run = step
+            if which == 1:
+                snap, held = eng.snapshot_state(), eng.packed.len.clone()
+                step()
+                eng.restore_state(snap)
+                eng.packed.len.copy_(held)
+                torch.cuda.synchronize()
+                run = eng.capture(step).replay
+            for _ in range(70):
+                run()
+                torch.cuda.synchronize()
+                logs[which].append((logits.clone(), eng.seq_len.tolist(), eng.packed.len.tolist(), eng.out_tokens.clone()))
+            eng.check_device_status()
+    for a, b in zip(*logs):
+        assert torch.equal(a[0], b[0]) and a[1] == b[1] and a[2] == b[2] and torch.equal(a[3], b[3])
+    P, n4 = logs[0][-1][1], logs[0][-1][2]
+    assert n4 == [max(0, p - 64) // PAGE * PAGE for p in P] and n4[0] >= 192
+    assert torch.equal(engs[0].packed.pool, engs[1].packed.pool)
+
+
+@pytest.mark.gpu
+def test_truncation_into_the_packed_part():
+    """Unpack, truncate, go on: the length held falls with the sequence, and stale 4-bit pages are not read."""
+    from paper_2609_00355_b200.binding import PackedCache
+    cache = Cache(H7, [700, 300], 1, 31)
+    eng = cache.eng
+    eng.glance_set_packed(PackedCache(eng))
+    eng.glance_pack_cache()
+    before = eng.kv_pool.clone()
+    new_len = torch.tensor([200, 1 << 20], dtype=torch.int32, device="cuda")
+    eng.glance_unpack_cache(new_len)
+    assert eng.packed.len.tolist() == [192, 256]
+    eng.glance_seq_truncate(0, 150, 0)
+    eng.check_device_status()
+    assert eng.packed.len.tolist() == [128, 256] and eng.seq_len.tolist() == [150, 300]
+    assert torch.equal(torch.isnan(eng.kv_pool), torch.isnan(before))
+    # new rows from position 150 on, in bf16
+    cache.lens = [150, 300]
+    for s, P in enumerate(cache.lens):
+        K, V = eng.gather_kv(s, 0, P + 1)
+        n = eng.packed.len.tolist()[s]
+        cache.K[s], cache.V[s] = K.double(), V.double()
+        cache.K[s][:n], cache.V[s][:n] = held_values(before_rows(before, eng, s, n)[0]), held_values(before_rows(before, eng, s, n)[1])
+    run_attention(cache, "block", 0, 0, 1, hide=False)
+    # a sequence that its owner shortened without a word: whole pages beyond it count for nothing
+    eng.seq_len.fill_(100)
+    cache.lens = [100, 100]
+    cache.K = [k[:101] for k in cache.K]
+    cache.V = [v[:101] for v in cache.V]
+    for s in range(2):
+        K, V = eng.gather_kv(s, 0, 101)
+        cache.K[s][64:], cache.V[s][64:] = K[64:].double(), V[64:].double()
+    run_attention(cache, "block", 0, 0, 1, hide=False)
+
+
+def before_rows(pool, eng, s, n):
+    pos = torch.arange(n, device="cuda")
+    pages = eng.page_table[s].long()[pos // PAGE]
+    return pool[0][pages, 0, :, pos % PAGE], pool[0][pages, 1, :, pos % PAGE]
+
+
+# ---- refusals, faults -------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_refusals():
+    from paper_2609_00355_b200.binding import GlanceError, PackedCache
+    eng = make_engine(HS, 2, 300)
+    q = torch.zeros(2 * 200, 16 * 64, dtype=torch.bfloat16, device="cuda")
+    anc = torch.ones(2, 4, 1, dtype=torch.int64, device="cuda")
+
+    def refused(what, fn):
+        with pytest.raises(GlanceError, match=what):
+            fn()
+    call = lambda T=4, layer=0, **kw: eng.glance_attention(layer, q[: 2 * T], T, q[: 2 * T].clone(), **kw)
+    refused("invalid argument", lambda: call(T=130))                       # a block of more than 128 rows
+    refused("invalid argument", lambda: call(layer=1))
+    refused("invalid argument", lambda: call(layer=-1))
+    refused("invalid argument", lambda: call(window=-1))
+    refused("invalid argument", lambda: call(sinks=-1))
+    refused("invalid argument", lambda: call(anc=anc, causal=True))
+    lib, ref, p = eng.lib, C.byref(eng.seqs), q.data_ptr()
+    for args in ((0, None, None, None, 1, 0, 0, 0, p, None), (0, p, None, None, 1, 0, 0, 0, None, None), (0, p + 2, None, None, 1, 0, 0, 0, p, None),
+                 (0, p, None, None, 0, 0, 0, 0, p, None), (0, p, None, None, 5000, 1, 0, 0, p, None), (0, p, p + 8, None, 1, 0, 0, 0, p, None)):
+        assert lib.glance_attention(eng.ctx, ref, *args) == -1
+    assert lib.glance_attention(eng.ctx, None, 0, p, None, None, 1, 0, 0, 0, p, None) == -1
+    refused("call order", lambda: eng.glance_pack_cache())
+    refused("call order", lambda: eng.glance_unpack_cache(torch.zeros(2, dtype=torch.int32, device="cuda")))
+    eng.glance_set_packed(PackedCache(eng))
+    refused("invalid argument", lambda: eng.glance_pack_cache(keep=-1))
+    assert lib.glance_unpack_cache(eng.ctx, ref, None) == -1
+    refused("one window", lambda: eng.glance_set_window([1, 2]))
+    refused("invalid argument", lambda: eng.glance_set_window([-1]))
+    refused("invalid argument", lambda: eng.glance_set_window([1], -1))
+    bad = PackedCache(eng)
+    for field in ("len", "page_table", "pool"):
+        c = type(bad.c).from_buffer_copy(bad.c)
+        setattr(c, field, None)
+        assert lib.glance_set_packed(eng.ctx, C.byref(c)) == -1
+    c = type(bad.c).from_buffer_copy(bad.c)
+    c.pool += 8
+    assert lib.glance_set_packed(eng.ctx, C.byref(c)) == -1
+    c = type(bad.c).from_buffer_copy(bad.c)
+    c.n_pages = 0
+    assert lib.glance_set_packed(eng.ctx, C.byref(c)) == -1
+    eng.glance_set_packed(None)
+    refused("call order", lambda: eng.glance_pack_cache())
+    call(T=4, anc=anc)
+    eng.check_device_status()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 40])
+def test_bad_pages_are_reported(T):
+    """Page numbers outside a pool are recorded in the status word; nothing outside the pools is read or written."""
+    for break_table in ("bf16", "held"):
+        cache = Cache(H7, [500], T, 3, held=200)
+        eng = cache.eng
+        if break_table == "bf16":
+            eng.page_table[0, -1] = eng.n_pages
+            eng.page_table[0, 500 // PAGE] = -1
+        else:
+            cache.packed.page_table[0, 2] = cache.packed.n_pages + 5
+        out = torch.empty_like(cache.q)
+        eng.glance_attention(0, cache.q, T, out)
+        assert eng.glance_poll_status() == -6
+        # packing pages that are nowhere: reported, the others move
+        eng.packed.len.zero_()
+        eng.glance_pack_cache(keep=0)
+        assert eng.glance_poll_status() == -6
+
+
+@pytest.mark.gpu
+def test_contexts_share_nothing_and_another_stream():
+    """Two engines on two streams at once: each has its own workspace."""
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    caches = []
+    for k, st in enumerate(streams):
+        with torch.cuda.stream(st):
+            caches.append(Cache(H7, [3000, 700], 2, 40 + k, held=64, stream=st))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(20):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                o = torch.empty_like(caches[k].q)
+                caches[k].eng.glance_attention(0, caches[k].q, 2, o, window=1000 * k)
+                outs[k].append(o)
+    torch.cuda.synchronize()
+    for k, st in enumerate(streams):
+        with torch.cuda.stream(st):
+            want = run_attention(caches[k], "block", 1000 * k, 0, 1, hide=False)
+            assert all(torch.equal(want, o) for o in outs[k])
+
+
+# ---- without a GPU ------------------------------------------------------------------------------------------------------
+def test_host_arguments_and_sizes():
+    from paper_2609_00355_b200 import binding
+    from paper_2609_00355_b200 import build as glance_build
+    glance_build.build()
+    lib = binding.load_library()
+    assert lib.glance_set_window(None, None, 0) == -1
+    assert lib.glance_set_packed(None, None) == -1
+    assert lib.glance_pack_cache(None, None, 0) == -1
+    assert lib.glance_unpack_cache(None, None, None) == -1
+    assert lib.glance_attention(None, None, 0, None, None, None, 1, 0, 0, 0, None, None) == -1
+    for name, d in (("7b", 128), ("small", 64)):
+        cfg = synth.CONFIGS[name]
+        cc = binding.make_config(cfg, 1, 100)
+        assert lib.glance_packed_bytes(C.byref(cc), 7) == cfg.n_layers * 7 * cfg.n_kv_heads * 2 * 64 * (d // 2 + d // 16)
+        assert lib.glance_packed_bytes(C.byref(cc), 0) == 0
+    assert lib.glance_packed_bytes(None, 3) == 0
+    cc.page_size = 32
+    assert lib.glance_packed_bytes(C.byref(cc), 7) == 0
+
+
+def test_definition_of_the_four_bit_values():
+    """The reference of these tests on values whose result is plain: ties, saturation, zeros, groups that are not finite."""
+    x = torch.zeros(8, 16)
+    x[0] = torch.tensor([6.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -0.75, -5.0, 0.26, 0.24, 4.9, 5.1, 0.0])      # scale 1
+    x[1, 0] = 6 * 17 / 16                                # scale between 1 and 1.125: the even code, 1
+    x[2, 0] = 1e9                                        # scale 448
+    x[3, 0] = 2.0 ** -10                                 # scale below half the smallest
+    x[4, :2] = torch.tensor([math.inf, 1.0])
+    x[5, :2] = torch.tensor([math.nan, 1.0])
+    v = held_values(x)
+    assert v[0].tolist() == [6.0, 0.0, 1.0, 1.0, 2.0, 2.0, 4.0, 4.0, 0.0, -1.0, -4.0, 0.5, 0.0, 4.0, 6.0, 0.0]
+    assert float(v[1, 0]) == 6.0 and float(v[2, 0]) == 2688.0 and float(v[3].abs().max()) == 0.0
+    assert bool(torch.isnan(v[4]).all()) and bool(torch.isnan(v[5]).all())
+    assert torch.equal(v[:4].float().to(torch.bfloat16).double(), v[:4])                                    # exact in bf16
