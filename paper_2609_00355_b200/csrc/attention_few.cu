@@ -40,7 +40,7 @@ constexpr int kEven = 6;
 // (codes, first products, softmax, second products) is long, and only other warps' pages hide it.
 template <int D, int NB>
 struct Few {
-    static constexpr int TEAMS = NB == 1 ? 3 : NB == 2 ? 2 : 1;
+    static constexpr int TEAMS = NB == 1 ? 3 : 2;
     static constexpr int WARPS = TEAMS * kTeam;              // consumers; one more fetches
     static constexpr int THREADS = (WARPS + TEAMS) * 32;
     // A team has a ring of its own, filled by a warp of its own (a thread that waits, announces and copies takes 270 ns a
@@ -48,7 +48,7 @@ struct Few {
     // swizzle), each of which takes three 4-bit tiles in its thirds; a bf16 page goes to a whole place.
     static constexpr int PAGE_BYTES = 2 * kPage * D * 2;
     static constexpr int THIRD = PAGE_BYTES / 3 / 16 * 16;
-    static constexpr int PLACES = NB == 4 ? 4 : 2;           // a team
+    static constexpr int PLACES = 2;                         // a team
     static constexpr int SLOTS = 3 * PLACES;
     static constexpr int RING = TEAMS * PLACES * PAGE_BYTES;
     static constexpr int ROWF = D + 4;
@@ -919,7 +919,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                     float acc[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-                    constexpr int U = NB == 4 ? 12 : 7;      // parts in flight
+                    constexpr int U = 7;                     // parts in flight
                     for (int c0 = team; c0 < parts; c0 += U * F::TEAMS) {
                         float2 ml[U];
                         float4 a[U][2];
@@ -1014,11 +1014,11 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStrea
 bool attention_few_takes(int T, int G) { return (long long)T * G <= kFewRows; }
 
 cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
-    const int rows = p.T * (p.Hq / p.Hkv), blocks = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
+    const int rows = p.T * (p.Hq / p.Hkv);
     auto pick = [&](auto d, auto two) {
         constexpr int D = decltype(d)::value;
         constexpr bool TWO = decltype(two)::value;
-        return blocks == 1 ? launch_few<D, 1, TWO>(p, map_kv, st) : blocks == 2 ? launch_few<D, 2, TWO>(p, map_kv, st) : launch_few<D, 4, TWO>(p, map_kv, st);
+        return rows <= 8 ? launch_few<D, 1, TWO>(p, map_kv, st) : launch_few<D, 2, TWO>(p, map_kv, st);
     };
     using D128 = std::integral_constant<int, 128>;
     using D64 = std::integral_constant<int, 64>;

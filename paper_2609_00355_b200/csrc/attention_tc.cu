@@ -40,6 +40,8 @@
 //   so everything after that is the same.  An operand tile is full when the copies and its warps are.  A ring of raw
 //   tiles filled by bulk copies was slower: what the producer thread does for a tile costs it 1.6 us beside the softmax
 //   warps (64 rows over 8704 positions 49 us).
+#include <algorithm>
+
 #include "kernels.cuh"
 #include "packed.cuh"
 #include "tc_ptx.cuh"
@@ -115,7 +117,7 @@ struct Smem {
 struct alignas(8) AttnBars {
     uint64_t q_ready, k_full[NG], k_empty[NG], v_full[NG], v_empty[NG], s_full[NG], p_full[NG], all_done, v_zero[NG], merge;
     uint32_t tmem_base;
-    int abort_flag;
+    int abort_flag, last;
 };
 
 template <int D, int CACHE>
@@ -143,7 +145,9 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         qt = (int)gridDim.x - 1 - i / p.Hkv;
         kvh = i % p.Hkv;
     }
-    const int s = blockIdx.z / p.S, split = blockIdx.z % p.S;
+    // key splits: p.S in a cluster, and (CACHE) several clusters a tile
+    const int n_splits = CACHE ? p.S * p.clusters : p.S;
+    const int s = blockIdx.z / n_splits, split = blockIdx.z % n_splits;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;     // (a uniform value to the compiler)
 
     if (threadIdx.x == 0) {
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         mbar_init(&bars.merge, 1);
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if (p.S > 1) {
+        if (p.S > 1 || (CACHE && p.clusters > 1)) {
             // split merge: this CTA owns a band of the tile's rows and receives that band from each of the S CTAs
             const int rpc = (QT + p.S - 1) / p.S;
             const int mine = max(0, min(rpc, QT - (int)cluster_rank() * rpc));
@@ -197,8 +201,8 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
     const int held = CACHE == kHeld ? min(max(p.held_len[s], 0), P) / kPage : 0;      // pages below this one come from the 4-bit pool
     // ceil-distribution of pages: the extra ones go to the first splits, because the last split already carries the
     // costlier masked tiles and the partial page
-    const int pg_begin = (int)(((long long)split * n_pages + p.S - 1) / p.S);
-    const int pg_end = (int)(((long long)(split + 1) * n_pages + p.S - 1) / p.S);
+    const int pg_begin = (int)(((long long)split * n_pages + n_splits - 1) / n_splits);
+    const int pg_end = (int)(((long long)(split + 1) * n_pages + n_splits - 1) / n_splits);
     const int np = pg_end - pg_begin;                    // pages of this CTA
     const int nt = (np + 1) / 2;                         // tiles, the last one may have one page only
     // half h of tile i: its page, and (kHeld) whether that is held in 4 bits
@@ -734,7 +738,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         if (trace && threadIdx.x == 64) trace[7] = global_ns();
         // ---------------- epilogue ----------------
         constexpr int OC = D / ECG;                       // output columns of a thread
-        if (p.S == 1) {
+        if (p.S == 1 && (!CACHE || p.clusters == 1)) {
             const float inv = CACHE && l_row == 0.f ? 0.f : 1.f / l_row;      // a row that sees nothing
             const bool aligned = (((uintptr_t)p.out | (uintptr_t)p.out_lo) & 15) == 0;     // (rows start on multiples of 128 bytes)
             const size_t off = ((size_t)(s * p.T + node) * p.Hq + kvh * G + g) * D + grp * OC;
@@ -810,6 +814,9 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
             cluster_arrive();
             if (trace && threadIdx.x == 64) trace[10] = global_ns();
             const float *rows = reinterpret_cast<const float *>(recv);
+            // CACHE, several clusters a tile: rows of this CTA's band in part `split / p.S` of the tile's parts
+            const size_t tile_id = ((size_t)s * p.Hkv + kvh) * gridDim.x + qt;
+            const size_t part_row = (tile_id * p.clusters + split / p.S) * QT + row_lo;
             const int my_rows = got ? max(0, min(own_rows, PR - qt * QT - row_lo)) : 0;
             constexpr int SEG = D / 8;                    // items per row: two 4-float pieces, half a row apart
 #pragma unroll 1
@@ -843,6 +850,15 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                     acc.x += ws * va[sp].x; acc.y += ws * va[sp].y; acc.z += ws * va[sp].z; acc.w += ws * va[sp].w;
                     bcc.x += ws * vb[sp].x; bcc.y += ws * vb[sp].y; bcc.z += ws * vb[sp].z; bcc.w += ws * vb[sp].w;
                 }
+                if constexpr (CACHE != kWhole) {
+                    if (p.clusters > 1) {                // this cluster's part of the row
+                        const size_t at = part_row + lr;
+                        *reinterpret_cast<float4 *>(p.parts + at * D + c0) = acc;
+                        *reinterpret_cast<float4 *>(p.parts + at * D + c1) = bcc;
+                        if (c0 == 0) reinterpret_cast<float2 *>(p.parts_ml)[at] = make_float2(M, den);
+                        continue;
+                    }
+                }
                 const float inv = CACHE && den == 0.f ? 0.f : 1.f / den;
                 const int prr = qt * QT + row_lo + lr;
                 const size_t off = ((size_t)(s * p.T + prr / G) * p.Hq + kvh * G + prr % G) * D;
@@ -851,12 +867,67 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                 store_two_term(p.out + off + c1, p.out_lo ? p.out_lo + off + c1 : nullptr,
                                make_float4(bcc.x * inv, bcc.y * inv, bcc.z * inv, bcc.w * inv));
             }
+            if constexpr (CACHE != kWhole) {
+                if (p.clusters > 1) {
+                    // The clusters' parts of a band meet in global memory; the CTA that comes last adds them in order.
+                    asm volatile("bar.sync 1, %0;" ::"n"(NSOFT) : "memory");
+                    int *last = &bars.last;
+                    if (tsm == 0) {
+                        // releases what the CTA wrote (the barrier orders it before this thread), acquires the others' parts
+                        int before;
+                        int32_t *counter = p.part_counters + tile_id * p.S + rank;
+                        __threadfence();
+                        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+                        *last = before == p.clusters - 1;
+                        if (*last) *counter = 0;         // for the next launch
+                    }
+                    asm volatile("bar.sync 1, %0;" ::"n"(NSOFT) : "memory");
+                    const int add_rows = *last ? max(0, min(own_rows, PR - qt * QT - row_lo)) : 0;
+#pragma unroll 1
+                    for (int item = tsm; item < add_rows * (D / 4); item += NSOFT) {
+                        const int lr = item / (D / 4), c0 = item % (D / 4) * 4;
+                        float M = -INFINITY, den = 0.f;
+                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                        constexpr int U = 8;             // parts in flight
+#pragma unroll 1
+                        for (int k0 = 0; k0 < p.clusters; k0 += U) {
+                            float2 ml[U];
+                            float4 a[U];
+#pragma unroll
+                            for (int k = 0; k < U; ++k) {
+                                const size_t at = (tile_id * p.clusters + min(k0 + k, p.clusters - 1)) * QT + row_lo + lr;
+                                ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.parts_ml) + at);
+                                a[k] = __ldcg(reinterpret_cast<const float4 *>(p.parts + at * D + c0));
+                            }
+                            float M2 = M;
+#pragma unroll
+                            for (int k = 0; k < U; ++k) {
+                                if (k0 + k >= p.clusters) ml[k].x = -INFINITY;
+                                M2 = fmaxf(M2, ml[k].x);
+                            }
+                            const float f0 = M == -INFINITY ? 0.f : ex2_approx(M - M2);
+                            den *= f0; acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+#pragma unroll
+                            for (int k = 0; k < U; ++k) {
+                                const float f = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - M2);
+                                den += f * ml[k].y;
+                                acc.x += f * a[k].x; acc.y += f * a[k].y; acc.z += f * a[k].z; acc.w += f * a[k].w;
+                            }
+                            M = M2;
+                        }
+                        const float inv = den == 0.f ? 0.f : 1.f / den;
+                        const int prr = qt * QT + row_lo + lr;
+                        const size_t off = ((size_t)(s * p.T + prr / G) * p.Hq + kvh * G + prr % G) * D + c0;
+                        store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+                    }
+                }
+            }
         }
         tc_fence_before();
     }
     if (trace && threadIdx.x == 64) trace[11] = global_ns();
     if (p.trace && threadIdx.x == 64) atomicMax(p.trace + 15, (unsigned long long)global_ns());  // grid span: last end
-    if (p.S > 1) {
+    if (p.S > 1 || (CACHE && p.clusters > 1)) {
         __syncwarp();
         if (warp < 2 || (CACHE && warp >= 2 + NSOFT / 32)) {     // the two arrivals of the softmax warps' merge
             cluster_arrive();
@@ -954,9 +1025,26 @@ cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, 
     return launch_d<64, kWhole>(p, map_kv, grid, st);
 }
 
+// Splits and clusters a tile for a cache that is read in part or held in 4 bits.  As attention_tc_splits; where a launch has few
+// tiles and `pages` (as many as a row may see) leave a CTA more than 12 of them, every tile gets as many clusters of four as fit at
+// once, whose parts meet in global memory (3 to 4 us): 28 rows over 32000 positions 122 us with one cluster of eight a kv head.
+void attention_cache_splits(AttnParams &p, long long pages) {
+    p.S = attention_tc_splits(p.T, p.Hq / p.Hkv, p.Hkv, p.batch, p.d);
+    p.clusters = 1;
+    const int tiles = attention_tc_q_tiles(p.T, p.Hq / p.Hkv) * p.Hkv * p.batch;
+    if (p.S < MAX_SPLITS || pages <= 12 * MAX_SPLITS) return;
+    constexpr int S = 4;
+    const int fit = (p.d == 128 ? max_active_clusters<128>(S) : max_active_clusters<64>(S)) / tiles;
+    const int n = (int)std::min<long long>(fit, (pages + 4 * S - 1) / (4 * S));       // four pages a CTA at least
+    if (n * S > p.S && (long long)tiles * n * QT <= kPartRows) {
+        p.S = S;
+        p.clusters = n;
+    }
+}
+
 cudaError_t launch_attention_cache(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
     const int G = p.Hq / p.Hkv;
-    dim3 grid(attention_tc_q_tiles(p.T, G), p.Hkv, p.batch * p.S);
+    dim3 grid(attention_tc_q_tiles(p.T, G), p.Hkv, p.batch * p.S * p.clusters);
     if (p.held_len) return p.d == 128 ? launch_d<128, kHeld>(p, map_kv, grid, st) : launch_d<64, kHeld>(p, map_kv, grid, st);
     return p.d == 128 ? launch_d<128, kWindow>(p, map_kv, grid, st) : launch_d<64, kWindow>(p, map_kv, grid, st);
 }

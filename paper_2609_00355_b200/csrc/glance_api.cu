@@ -71,8 +71,8 @@ struct Workspace {
     unsigned long long *tk_cand;   // [vocab tiles][batch*B][kTopkTileCap]
     float *wide_planes;            // partial tiles of gemm_wide_kernel, or nullptr where its rule never chooses it
     int32_t *wide_counters;        // [kWideCut][2], zero between launches
-    float *few_parts, *few_ml;     // attention of few rows: partial results [kFewParts][kFewRows][d] and [..][2]
-    int32_t *few_counters;         // [max_batch * Hkv], zero between launches
+    float *part_rows, *part_ml;    // attention whose splits meet in global memory: [kPartRows][d] and [kPartRows][2]
+    int32_t *part_counters;        // zero between launches
     int32_t *pack_counter;         // zero between launches
     size_t total;
 };
@@ -92,6 +92,8 @@ Dims make_dims(const glance_config &c) {
     d.n_ssq = (c.hidden + 127) / 128;
     return d;
 }
+
+size_t part_counters(const glance_config &c) { return std::max<size_t>((size_t)c.max_batch * c.n_kv_heads, kPartCounters); }
 
 // carve (or just size, when base == nullptr) the workspace
 Workspace carve(const glance_config &c, const Dims &d, unsigned char *base) {
@@ -135,9 +137,9 @@ Workspace carve(const glance_config &c, const Dims &d, unsigned char *base) {
     }
     w.wide_planes = wide ? (float *)take(kWidePlaneFloats * 4) : nullptr;
     w.wide_counters = (int32_t *)take((size_t)kWideCut * 2 * 4);
-    w.few_parts = (float *)take((size_t)kFewParts * kFewRows * c.head_dim * 4);
-    w.few_ml = (float *)take((size_t)kFewParts * kFewRows * 2 * 4);
-    w.few_counters = (int32_t *)take((size_t)c.max_batch * c.n_kv_heads * 4);
+    w.part_rows = (float *)take((size_t)kPartRows * c.head_dim * 4);
+    w.part_ml = (float *)take((size_t)kPartRows * 2 * 4);
+    w.part_counters = (int32_t *)take(part_counters(c) * 4);
     w.pack_counter = (int32_t *)take(4);
     w.total = off;
     return w;
@@ -304,11 +306,16 @@ void attention_cache(glance_ctx *ctx, AttnParams ap, int layer, int seq_off) {
         ap.held_pages = ctx->held.n_pages;
         ap.held_layer = (const unsigned char *)ctx->held.pool + (size_t)layer * ctx->held.n_pages * c.n_kv_heads * packed::tile_bytes(c.head_dim);
     }
-    ap.parts = ctx->ws.few_parts; ap.parts_ml = ctx->ws.few_ml; ap.part_counters = ctx->ws.few_counters;
+    ap.parts = ctx->ws.part_rows; ap.parts_ml = ctx->ws.part_ml; ap.part_counters = ctx->ws.part_counters;
     const CUtensorMap *m = get_map(ctx, ap.pool_layer, ap.d, ap.geom.n_pages * 2 * ap.geom.n_kv_heads * kPage, kPage);
     if (!m) return;
     const bool few = attention_few_takes(ap.T, ap.Hq / ap.Hkv);
-    if (!few) ap.S = attention_tc_splits(ap.T, ap.Hq / ap.Hkv, ap.Hkv, ap.batch, ap.d);
+    if (!few) {
+        // pages that a row may see: the lengths themselves are on the device
+        long long pages = c.max_pages_per_seq;
+        if (ap.window > 0) pages = std::min(pages, ((long long)ap.window + ap.T + kPage - 1) / kPage + 1 + ((long long)ap.sinks + kPage - 1) / kPage);
+        attention_cache_splits(ap, pages);
+    }
     const bool prof = prof_begin(ctx);
     if ((few ? launch_attention_few(ap, *m, ctx->stream) : launch_attention_cache(ap, *m, ctx->stream)) != cudaSuccess) ctx->map_error = true;
     prof_end(ctx, prof, KIND_ATTN, 0.0);
@@ -571,7 +578,7 @@ int32_t glance_create(const glance_config *cfg, const glance_target_weights *t, 
         cudaMemsetAsync(ws.am_keys, 0, (size_t)d.Rlog * 8, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.am_counter, 0, 256, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.wide_counters, 0, (size_t)kWideCut * 2 * 4, ctx->stream) != cudaSuccess ||
-        cudaMemsetAsync(ws.few_counters, 0, (size_t)cfg->max_batch * cfg->n_kv_heads * 4, ctx->stream) != cudaSuccess ||
+        cudaMemsetAsync(ws.part_counters, 0, part_counters(*cfg) * 4, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.pack_counter, 0, 4, ctx->stream) != cudaSuccess ||
         cudaMemsetAsync(ws.tk_thr, 0, (size_t)cfg->max_batch * cfg->block_B * kTopkTileCap * 4, ctx->stream) != cudaSuccess) {
         delete ctx;

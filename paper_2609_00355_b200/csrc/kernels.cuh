@@ -148,17 +148,20 @@ struct AttnParams {
     const unsigned char *held_layer;   // (page, kv head) tiles of packed.cuh
     const int32_t *held_table;   // [batch][max_pages_per_seq]
     int held_pages;
-    float *parts, *parts_ml;     // workspace: [2 * CTAs][kFewRows][d], [..][kFewRows][2]
-    int32_t *part_counters;      // [batch * Hkv], zero between launches
+    int clusters;                // of S key splits a tile (launch_attention_cache)
+    float *parts, *parts_ml;     // workspace: [kPartRows][d] unnormalised outputs, [kPartRows][2] their (maximum, sum)
+    int32_t *part_counters;      // [max(batch * Hkv, kPartCounters)], zero between launches
 };
 // few query rows over a cache read in part: at most kFewRows packed rows (T * heads of a kv head)
-constexpr int kFewRows = 32;
-constexpr int kFewParts = 2 * 148;           // partial results of a launch: two a CTA, one CTA an SM
+constexpr int kFewRows = 16;
+constexpr int kPartRows = 2 * 148 * kFewRows;        // partial results of a launch: two a CTA, one CTA an SM
+constexpr int kPartCounters = 256;
 bool attention_few_takes(int T, int G);
 cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 // map_kv = 2-D map of the pool layer {d, n_pages*2*Hkv*64 rows}, box {64, 64}
 cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 // the same for a cache that is read in part or held in 4 bits (window, sinks, held_*)
+void attention_cache_splits(AttnParams &p, long long pages);
 cudaError_t launch_attention_cache(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 CtaSize attention_tc_cta_size(int d);
 int attention_tc_q_tiles(int T, int G);

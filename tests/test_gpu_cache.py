@@ -648,3 +648,27 @@ def test_definition_of_the_four_bit_values():
     assert float(v[1, 0]) == 6.0 and float(v[2, 0]) == 2688.0 and float(v[3].abs().max()) == 0.0
     assert bool(torch.isnan(v[4]).all()) and bool(torch.isnan(v[5]).all())
     assert torch.equal(v[:4].float().to(torch.bfloat16).double(), v[:4])                                    # exact in bf16
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,kind,T,lens,window,sinks,held", [
+    (H7, "tree", 4, [7000], 0, 0, 64), (H7, "tree", 5, [20000], 19000, 100, None), (HS, "tree", 8, [9000], 0, 0, 5000), (H7, "tree", 18, [6500], 6300, 0, 64),
+    ((16, 1, 64), "block", 3, [30000], 0, 0, 0), (H7, "tree", 4, [100], 0, 0, 0), ((8, 8, 128), "tree", 30, [7000], 0, 0, 3000),
+    (H7, "chain", 20, [9000], 8500, 7, 300), (HT, "block", 16, [40000], 0, 0, 64)])
+def test_tiles_split_over_several_clusters(heads, kind, T, lens, window, sinks, held):
+    """Few tiles over a long table: every tile's clusters meet in global memory.  Also where the sequence is much shorter than the
+    table, so that most clusters have nothing."""
+    cache = Cache(heads, lens + ([] if lens[0] > 5000 else [7000]), T, 51, held=held)
+    run_attention(cache, kind, window, sinks, 8)
+    run_attention(cache, kind, window, sinks, 9, two=True, hide=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,lens,window,sinks,held", [
+    (H7, [33000], 0, 0, 64), (H7, [5000 + 37 * i for i in range(16)], 0, 0, 100), (H7, [1, 0, 9000, 64, 63, 128], 4000, 70, 64), (HS, list(range(64)), 20, 2, 0),
+    ((32, 8, 128), [3000 - 41 * i for i in range(20)], 0, 0, None), ((8, 8, 128), [12000, 1], 11000, 0, None), ((16, 1, 64), [50, 20000, 7], 0, 0, 3000)])
+def test_stretches_of_a_batch(heads, lens, window, sinks, held):
+    """Single tokens of ragged batches: stretches that begin and end inside an item, items shared by many CTAs, even shares."""
+    cache = Cache(heads, lens, 1, 52, held=held)
+    run_attention(cache, "block", window, sinks, 8)
+    run_attention(cache, "block", window, sinks, 9, two=True, hide=False)
