@@ -273,8 +273,9 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         if (lane == 0) bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (!p.early) pdl_wait();
     if (warp == 1) {
-        // lengths may be read before the dependency wait: see attention_tc.cu
+        // (inside a pass lengths may be read before the dependency wait: see attention_tc.cu)
         int run = 0, most = 0;
         for (int s0 = 0; s0 < p.batch; s0 += 32) {
             int n = 0;

@@ -413,7 +413,7 @@ void run_layer(glance_ctx *ctx, int layer, const LayerW &w, bf16 *pool_layer, co
     ap.lo_skip = ctx->attn_lo_skip; ap.lo_skip_min_keys = ctx->attn_lo_min_keys;
     const int window = layer >= 0 && !ctx->window.empty() ? ctx->window[layer] : 0;
     if (window > 0 || (layer >= 0 && ctx->held.pool)) {
-        ap.window = window; ap.sinks = window > 0 ? ctx->sinks : 0;
+        ap.window = window; ap.sinks = window > 0 ? ctx->sinks : 0; ap.early = 1;
         attention_cache(ctx, ap, layer, ps.seq_off);
     } else {
         ap.S = attention_tc_splits(ps.T, c.n_q_heads / c.n_kv_heads, c.n_kv_heads, ps.batch, c.head_dim);

@@ -148,6 +148,7 @@ struct AttnParams {
     const unsigned char *held_layer;   // (page, kv head) tiles of packed.cuh
     const int32_t *held_table;   // [batch][max_pages_per_seq]
     int held_pages;
+    int early;                   // 1: lengths, page tables and committed rows may be read before the dependency wait (inside a pass)
     int clusters;                // of S key splits a tile (launch_attention_cache)
     float *parts, *parts_ml;     // workspace: [kPartRows][d] unnormalised outputs, [kPartRows][2] their (maximum, sum)
     int32_t *part_counters;      // [max(batch * Hkv, kPartCounters)], zero between launches

@@ -672,3 +672,58 @@ def test_stretches_of_a_batch(heads, lens, window, sinks, held):
     cache = Cache(heads, lens, 1, 52, held=held)
     run_attention(cache, "block", window, sinks, 8)
     run_attention(cache, "block", window, sinks, 9, two=True, hide=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,T", [(H7, 2), (H7, 40), (HS, 3), (HS, 70)])
+def test_rows_that_see_nothing_are_zeros(heads, T):
+    """Empty sets over no context, in one call with rows that see something; and sets without the row itself."""
+    Hq, Hkv, d = heads
+    cache = Cache(heads, [0, 300], T, 61)
+    eng = cache.eng
+    W = (T + 63) // 64
+    anc = torch.zeros(2, T, W, dtype=torch.int64, device="cuda")
+    anc[0, 1, 0] = 1                                     # sequence 0: only row 1 sees anything: row 0
+    anc[1, :, 0] = 2                                     # sequence 1: everybody sees row 1 and a window of the context
+    out = torch.full_like(cache.q, 9.0)
+    eng.glance_attention(0, cache.q, T, out, anc=anc, window=50)
+    eng.check_device_status()
+    out = out.view(2, T, Hq, d)
+    assert float(out[0, [i for i in range(T) if i != 1]].abs().max()) == 0.0
+    assert torch.equal(out[0, 1].view(Hkv, -1, d).double(), cache.V[0][0][:, None].expand(-1, Hq // Hkv, -1))
+    see = np.zeros((T, 300 + T), dtype=bool)
+    see[:, 301] = True
+    see[:, 300 - 49 : 300] = True                        # a set of one stands at the first position
+    ref, A = reference(cache.q.view(2, T, Hq, d)[1].double(), cache.K[1], cache.V[1], see)
+    check(out[1], ref, A)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 30])
+def test_pools_beyond_four_gigabytes(T):
+    """Pages whose bytes lie beyond 2^32 in the bf16 pool of a layer and in the 4-bit pool."""
+    from paper_2609_00355_b200.binding import PackedCache
+    heads, P = H7, 1000
+    cache = Cache(heads, [P], T, 71)
+    big = make_engine(heads, 1, 40000 * PAGE)
+    assert big.kv_pool.numel() * 2 > 1 << 32
+    n = (P + T + PAGE - 1) // PAGE
+    pages = torch.arange(big.n_pages - n, big.n_pages, dtype=torch.int32, device="cuda")
+    big.page_table[0, :n] = pages
+    for p in range(n):
+        big.kv_pool[:, int(pages[p])] = cache.eng.kv_pool[:, int(cache.eng.page_table[0, p])]
+    big.seq_len.fill_(P)
+    packed = PackedCache(big, n_pages=130000)
+    assert packed.pool.numel() > 1 << 32
+    packed.page_table[0, :n] = torch.arange(130000 - n, 130000, dtype=torch.int32, device="cuda")
+    big.glance_set_packed(packed)
+    small, cache.eng = cache.eng, big
+    run_attention(cache, "tree", 700, 30, 2, hide=False)
+    big.glance_pack_cache(keep=100)
+    held = int(packed.len[0])
+    assert held == 896
+    cache.K[0][:held], cache.V[0][:held] = held_values(cache.K[0][:held]), held_values(cache.V[0][:held])
+    big.kv_pool[:, pages[: held // PAGE].long()] = math.nan
+    run_attention(cache, "tree", 0, 0, 2, hide=False)
+    big.glance_unpack_cache(torch.zeros(1, dtype=torch.int32, device="cuda"))
+    run_attention(cache, "tree", 0, 0, 2, hide=False)
