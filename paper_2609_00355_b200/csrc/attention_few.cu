@@ -35,6 +35,8 @@ constexpr int kTeam = 4;                     // consumer warps that share a page
 constexpr int kMaxSeqs = 64;
 constexpr float kRaise = 8.f;                // log2 units a score may exceed its reference by
 constexpr int kEven = 6;
+constexpr int kMaxCluster = 8;
+constexpr int kMorePages = 3;
 
 // NB: blocks of 8 query rows.  As many teams as the registers of NB blocks' accumulators leave room for: a page's chain
 // (codes, first products, softmax, second products) is long, and only other warps' pages hide it.
@@ -250,6 +252,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     __shared__ int upto[kMaxSeqs + 1];                       // pages (of all heads) of the sequences before
     __shared__ int lens[kMaxSeqs], helds[kMaxSeqs];          // positions; pages held in 4 bits
     __shared__ int most_pages[32];                           // of a (sequence, kv head)
+    __shared__ float sum_m[8 * NB], sum_l[8 * NB];           // clusters: this CTA's part of its item (the outputs: in `red`)
     __shared__ RowMask mask[8 * NB];
     __shared__ int pages[F::TEAMS][32];
     __shared__ float red_m[kWarps][8 * NB], red_l[kWarps][8 * NB];
@@ -272,6 +275,10 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         }
         if (lane == 0) bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < 8 * NB) {
+        sum_m[threadIdx.x] = -INFINITY;
+        sum_l[threadIdx.x] = 0.f;
     }
     if (!p.early) pdl_wait();
     if (warp == 1) {
@@ -300,15 +307,14 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         if (lane == 0) upto[0] = 0;
     }
     __syncthreads();
-    // ---- this CTA's stretch of the line: either equal stretches, which may begin and end inside an item ((sequence, kv head)),
-    // or, where that costs the longest item no more than kEven pages, the same number of CTAs for every item, so that a CTA
+    // ---- this CTA's stretch of the line: with clusters, a share of its cluster's item ((sequence, kv head)); else either equal stretches, which may begin and end inside an item, or, where that costs the longest item no more than kEven pages, the same number of CTAs for every item, so that a CTA
     // has one item to start and to finish (4 to 5 us each). ----
     const int total = upto[p.batch], items = p.batch * p.Hkv;
     int most = most_pages[lane];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-    int chunk = (total + (int)gridDim.x - 1) / (int)gridDim.x, per_item = (int)gridDim.x / items;
-    if (per_item > 0 && (most + per_item - 1) / per_item > chunk + kEven) per_item = 0;
+    int chunk = (total + (int)gridDim.x - 1) / (int)gridDim.x, per_item = p.S > 0 ? p.S : (int)gridDim.x / items;
+    if (p.S == 0 && per_item > 0 && (most + per_item - 1) / per_item > chunk + kEven) per_item = 0;
     int s = 0, x_begin, x_end;
     if (per_item > 0) {
         const int item = (int)blockIdx.x / per_item, sub = (int)blockIdx.x % per_item;
@@ -424,6 +430,10 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
             }
         }
         __syncwarp();
+        if (p.S > 0) {                                       // the two barriers of the clusters' merge
+            cluster_sync_all();
+            cluster_sync_all();
+        }
         return;
     }
 
@@ -840,7 +850,13 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         };
         auto emit = [&](int row, int d0, float M, float L, float4 acc) {
             if (row >= rows) return;
-            if (parts == 1) {
+            if (p.S > 0) {
+                *reinterpret_cast<float4 *>(red + row * F::ROWF + d0) = acc;
+                if (d0 == 0) {
+                    sum_m[row] = M;
+                    sum_l[row] = L;
+                }
+            } else if (parts == 1) {
                 const float inv = L > 0.f ? 1.f / L : 0.f;
                 const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
                 store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
@@ -897,7 +913,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
             }
         }
         if (trace) trace[6] = global_ns();
-        if (parts > 1) {
+        if (p.S == 0 && parts > 1) {
             asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
             if (tid == 0) {
                 // releases what the whole CTA wrote (the barrier orders it before this thread), acquires the others' parts
@@ -981,8 +997,74 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         }
         x += v1 - v0;
     }
+    if (p.S > 0) {
+        // ---- the cluster's CTAs hold a part of one item each: every CTA adds its share of the elements over all of them ----
+        __syncwarp();
+        cluster_sync_all();
+        if (trace) trace[8] = global_ns();
+        const int item = (int)blockIdx.x / p.S, sq = item / p.Hkv, kvh = item % p.Hkv;
+        const int n = min(PR, 8 * NB) * (D / 4);
+        for (int i = (int)cluster_rank() + p.S * tid; i < n; i += p.S * kWarps * 32) {
+            const int row = i / (D / 4), d0 = i % (D / 4) * 4;
+            float pm[kMaxCluster], pl[kMaxCluster], M = -INFINITY, L = 0.f;
+            float4 a[kMaxCluster], acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kMaxCluster; ++k) {
+                const uint32_t from = (uint32_t)min(k, p.S - 1);
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(pm[k]) : "r"(map_to_rank(smem_u32(sum_m + row), from)) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(pl[k]) : "r"(map_to_rank(smem_u32(sum_l + row), from)) : "memory");
+                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(a[k].x), "=f"(a[k].y), "=f"(a[k].z), "=f"(a[k].w)
+                             : "r"(map_to_rank(smem_u32(red + row * F::ROWF + d0), from)) : "memory");
+            }
+#pragma unroll
+            for (int k = 0; k < kMaxCluster; ++k)
+                if (k < p.S) M = fmaxf(M, pm[k]);
+#pragma unroll
+            for (int k = 0; k < kMaxCluster; ++k)
+                if (k < p.S && pm[k] != -INFINITY) {         // (a CTA without pages wrote no outputs)
+                    const float f = ex2(pm[k] - M);
+                    L += f * pl[k];
+                    acc.x += f * a[k].x; acc.y += f * a[k].y; acc.z += f * a[k].z; acc.w += f * a[k].w;
+                }
+            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const size_t off = ((size_t)(sq * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
+            store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+        }
+        __syncwarp();
+        cluster_sync_all();                                  // nobody leaves while a peer may read its part
+    }
     if (trace) trace[11] = global_ns();
     if (p.trace && threadIdx.x == 0) atomicMax(p.trace + 15, (unsigned long long)global_ns());
+}
+
+template <int D, int NB>
+cudaLaunchConfig_t few_config(cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(Few<D, NB>::THREADS, 1, 1);
+    cfg.dynamicSmemBytes = Few<D, NB>::TOTAL;
+    cfg.stream = st;
+    return cfg;
+}
+
+// clusters of S CTAs that are resident at once (queried once per size; the kernel's attributes are set)
+template <int D, int NB, bool TWO>
+int few_clusters(int S) {
+    static int cache[kMaxCluster + 1] = {0};
+    if (cache[S] == 0) {
+        cudaLaunchConfig_t cfg = few_config<D, NB>(nullptr);
+        cfg.gridDim = dim3(S, 1, 1);
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = S;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, attn_few_kernel<D, NB, TWO>, &cfg) != cudaSuccess || n < 1) n = 1;
+        cache[S] = n;
+    }
+    return cache[S];
 }
 
 template <int D, int NB, bool TWO>
@@ -994,20 +1076,30 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStrea
         if (e != cudaSuccess) return e;
         once = true;
     }
-    cudaLaunchConfig_t cfg = {};
-    // no more CTAs than pages that a row can see: the lengths themselves are on the device
+    // pages that a row can see (the lengths themselves are on the device)
     long long pages = p.geom.max_pages_per_seq;
     if (p.window > 0) pages = std::min(pages, ((long long)p.window + p.T + kPage - 1) / kPage + 1 + ((long long)p.sinks + kPage - 1) / kPage);
-    cfg.gridDim = dim3((unsigned)std::min<long long>(148, pages * p.Hkv * p.batch), 1, 1);
-    cfg.blockDim = dim3(F::THREADS, 1, 1);
-    cfg.dynamicSmemBytes = F::TOTAL;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    const int items = p.Hkv * p.batch;
+    // A cluster an item, whose CTAs add their parts through distributed shared memory in 1.5 us, where that costs a CTA no more
+    // than kMorePages pages (0.4 us in 4 bits, 0.8 in bf16) beyond its share of the line; there the parts of an item meet in
+    // global memory, 3.5 us and more.
+    AttnParams q = p;
+    q.S = 0;
+    for (int S = kMaxCluster; S > 1 && q.S == 0; S /= 2)
+        if (items <= few_clusters<D, NB, TWO>(S) && (pages + S - 1) / S <= (pages * items + 147) / 148 + kMorePages) q.S = S;
+    cudaLaunchConfig_t cfg = few_config<D, NB>(st);
+    // (no more CTAs than pages)
+    cfg.gridDim = dim3((unsigned)(q.S > 0 ? (long long)items * q.S : std::min<long long>(148, pages * items)), 1, 1);
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = q.S;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_few_kernel<D, NB, TWO>, map_kv, p);
+    cfg.numAttrs = q.S > 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, attn_few_kernel<D, NB, TWO>, map_kv, q);
 }
 
 }  // namespace

@@ -666,6 +666,7 @@ def test_tiles_split_over_several_clusters(heads, kind, T, lens, window, sinks, 
 @pytest.mark.gpu
 @pytest.mark.parametrize("heads,lens,window,sinks,held", [
     (H7, [33000], 0, 0, 64), (H7, [5000 + 37 * i for i in range(16)], 0, 0, 100), (H7, [1, 0, 9000, 64, 63, 128], 4000, 70, 64), (HS, list(range(64)), 20, 2, 0),
+    (H7, [40 * i for i in range(16)], 0, 0, None), (H7, [40 * i for i in range(16)], 0, 0, 64), (HS, [37 * i for i in range(7)], 100, 3, 64),
     ((32, 8, 128), [3000 - 41 * i for i in range(20)], 0, 0, None), ((8, 8, 128), [12000, 1], 11000, 0, None), ((16, 1, 64), [50, 20000, 7], 0, 0, 3000)])
 def test_stretches_of_a_batch(heads, lens, window, sinks, held):
     """Single tokens of ragged batches: stretches that begin and end inside an item, items shared by many CTAs, even shares."""
