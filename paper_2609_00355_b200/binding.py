@@ -371,23 +371,25 @@ class Engine:
 
     def glance_unpack_cache(self, new_len: torch.Tensor, kv_pool: Optional[torch.Tensor] = None):
         """Pages from new_len [batch] (int32, device) on back to bf16: into the engine's pool, or into another of its shape."""
-        assert new_len.dtype == torch.int32 and new_len.numel() == self.batch
-        if kv_pool is not None:
-            assert kv_pool.shape == self.kv_pool.shape and kv_pool.dtype == self.kv_pool.dtype
-            self.seqs.kv_pool = _ptr(kv_pool)
+        assert new_len.dtype is torch.int32 and new_len.numel() == self.batch, "new_len: int32, one a sequence"
+        if kv_pool is None:
+            _check(self.lib.glance_unpack_cache(self.ctx, C.byref(self.seqs), _ptr(new_len)), "glance_unpack_cache")
+            return
+        assert kv_pool.dtype is torch.bfloat16 and kv_pool.numel() == self.kv_pool.numel(), "kv_pool: the engine's shape"
+        own, self.seqs.kv_pool = self.seqs.kv_pool, _ptr(kv_pool)
         try:
             _check(self.lib.glance_unpack_cache(self.ctx, C.byref(self.seqs), _ptr(new_len)), "glance_unpack_cache")
         finally:
-            self.seqs.kv_pool = self.kv_pool.data_ptr()
+            self.seqs.kv_pool = own
 
     def glance_attention(self, layer: int, q: torch.Tensor, T: int, out: torch.Tensor, anc: Optional[torch.Tensor] = None,
                          causal: bool = False, window: int = 0, sinks: int = 0, q_lo: Optional[torch.Tensor] = None,
                          out_lo: Optional[torch.Tensor] = None):
         """Attention of T rows a sequence over layer `layer`'s cache (window, sinks, 4-bit pages): see glance.h."""
-        shape = self.batch * T * self.cfg.n_q_heads * self.cfg.head_dim
-        for x in (q, out, q_lo, out_lo):
-            assert x is None or (x.dtype == torch.bfloat16 and x.numel() == shape), "bf16 tensors of batch * T rows"
-        assert anc is None or (anc.dtype == torch.int64 and anc.numel() == self.batch * T * ((T + 63) // 64)), "anc: 64-bit words"
+        n = self.batch * T * self.ccfg.n_q_heads * self.ccfg.head_dim
+        for x in (q, out) if q_lo is None and out_lo is None else (q, out, q_lo, out_lo):
+            assert x is None or (x.dtype is torch.bfloat16 and x.numel() == n), "bf16 tensors of batch * T rows"
+        assert anc is None or (anc.dtype is torch.int64 and anc.numel() == self.batch * T * ((T + 63) // 64)), "anc: 64-bit words"
         _check(self.lib.glance_attention(self.ctx, C.byref(self.seqs), layer, _ptr(q), _ptr(q_lo), _ptr(anc), T, 1 if causal else 0,
                                          window, sinks, _ptr(out), _ptr(out_lo)), "glance_attention")
 

@@ -9,6 +9,7 @@
 
 #include "kernels.cuh"
 #include "packed.cuh"
+#include "tc_ptx.cuh"
 
 namespace glance {
 
@@ -31,19 +32,25 @@ __device__ __forceinline__ uint32_t scale_code(float a) {
     asm("{\n\t.reg .b16 x;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %1, %2;\n\tcvt.u32.u16 %0, x;\n\t}" : "=r"(r) : "f"(0.f), "f"(twelve));
     return r & 0xffu;
 }
-// e2m1 of x / s for two values (a in the low nibble), r = 1 / s rounded.  A quotient of an eight-bit and a four-bit
-// significand is a border of e2m1 (an odd multiple of 1/4, 1/2 or 1) exactly or at least 2^-10 away from one.  So it may be
-// rounded to a multiple of 2^-13, which undoes the rounding of r (one place: 2^-19 at most where it matters) and keeps ties ties.
-__device__ __forceinline__ uint32_t value_codes(float a, float b, float r) {
+// e2m1 of x / s for the eight values of four words, first value in the lowest nibble; r = 1 / s rounded.  A quotient of an eight-bit
+// and a four-bit significand is a border of e2m1 (an odd multiple of 1/4, 1/2 or 1) exactly or at least 2^-10 away from one.
+// So it may be rounded to a multiple of 2^-13, which undoes the rounding of r (one place: 2^-19 at most where it matters) and
+// keeps ties ties.
+__device__ __forceinline__ uint32_t value_codes(const uint32_t (&w)[4], float r) {
     constexpr float kGrid = 1536.f;                      // 1.5 * 2^10: its last place is 2^-13
-    const float qa = __fsub_rn(__fmaf_rn(a, r, kGrid), kGrid), qb = __fsub_rn(__fmaf_rn(b, r, kGrid), kGrid);
+    const float2 r2 = make_float2(r, r), up = make_float2(kGrid, kGrid), down = make_float2(-kGrid, -kGrid);
+    float2 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        q[i] = tc::add2(tc::fma2(make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), r2, up), down);
     uint32_t c;
-    asm("{\n\t.reg .b8 x;\n\t.reg .b16 y;\n\tcvt.rn.satfinite.e2m1x2.f32 x, %1, %2;\n\tmov.b16 y, {x, 0};\n\tcvt.u32.u16 %0, y;\n\t}" : "=r"(c) : "f"(qb), "f"(qa));
-    return c & 0xffu;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(c) : "f"(q[0].x), "f"(q[0].y), "f"(q[1].x), "f"(q[1].y), "f"(q[2].x), "f"(q[2].y), "f"(q[3].x), "f"(q[3].y));
+    return c;
 }
-
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // A group's 32 bytes of bf16 in one access: as two of 16 a warp's accesses would cover half of every sector each time.
 __device__ __forceinline__ void load32(const void *p, uint4 (&v)[2]) {
@@ -57,10 +64,10 @@ __device__ __forceinline__ void store32(void *p, const uint4 (&v)[2]) {
 
 // 16 bf16 values -> 8 bytes of codes and the scale's code
 __device__ __forceinline__ uint2 pack_group(const uint4 (&v)[2], uint32_t &scale) {
-    const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    const uint32_t w[2][4] = {{v[0].x, v[0].y, v[0].z, v[0].w}, {v[1].x, v[1].y, v[1].z, v[1].w}};
     uint32_t both = 0;                                   // the largest magnitude, by its bits
 #pragma unroll
-    for (int i = 0; i < 8; ++i) both = __vmaxu2(both, w[i] & 0x7fff7fffu);
+    for (int i = 0; i < 8; ++i) both = __vmaxu2(both, w[i >> 2][i & 3] & 0x7fff7fffu);
     const uint32_t top = max(both & 0xffffu, both >> 16);
     scale = top >= 0x7f80u ? 0x7fu : scale_code(__uint_as_float(top << 16));
     __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)scale, __NV_E4M3);
@@ -68,13 +75,8 @@ __device__ __forceinline__ uint2 pack_group(const uint4 (&v)[2], uint32_t &scale
     const bool live = s > 0.f;                           // a scale of 0 or NaN: codes 0
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
-    uint2 out = make_uint2(0u, 0u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t c = live ? value_codes(bf_lo(w[i]), bf_hi(w[i]), r) : 0u;
-        (i < 4 ? out.x : out.y) |= c << (8 * (i & 3));
-    }
-    return out;
+    const uint2 out = make_uint2(value_codes(w[0], r), value_codes(w[1], r));
+    return live ? out : make_uint2(0u, 0u);
 }
 
 __device__ __forceinline__ void unpack_group(uint2 c, uint32_t scale, uint4 (&v)[2]) {
