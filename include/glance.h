@@ -118,14 +118,17 @@ typedef struct {
  * nearest to max|x| / 6 (448 at most, 0 where that rounds to 0); a value is held as the e2m1 value (0, 0.5, 1, 1.5, 2, 3, 4, 6
  * and their negatives) nearest to x / s and stands for s times it; ties go to the even code.  That product is exact in bf16.
  * 16 values with an infinity or a NaN among them are held as NaN.  4.5 bits a value: 3.56 times less than bf16.
- * Positions [0, len[s]) of sequence s, whole pages, are read from `pool` in every target layer, later ones from kv_pool, whose
- * pages below len[s] are then not read by any pass (their entries in glance_seqs.page_table may name any page of the pool).
- * Only positions below seq_len are read here: of len[s], whole pages of it.  The block head's cache stays in bf16. */
+ * Positions [0, len[s]) of sequence s, whole pages, are read from `pool` in every target layer, later ones from kv_pool.
+ * Only positions below seq_len are read here: of len[s], whole pages of it.  The block head's cache stays in bf16 and goes through
+ * head_page_table, pages of a head_kv_pool of head_n_pages a layer; with it no pass looks at the entries of glance_seqs.page_table
+ * below len[s], so those pages of kv_pool can be given to other positions.  NULL: the head goes through glance_seqs.page_table. */
 typedef struct {
     int32_t n_pages;           /* pages in the pool (per layer) */
     int32_t *len;              /* device [max_batch]: positions held in 4 bits, multiples of page_size; 0 at the start */
     const int32_t *page_table; /* device [max_batch][max_pages_per_seq]: page of the pool that holds a sequence's page */
     void *pool;                /* device, 16-byte aligned, glance_packed_bytes(cfg, n_pages) bytes: (layer, page, kv_head) tiles */
+    const int32_t *head_page_table; /* device [max_batch][max_pages_per_seq], or NULL */
+    int32_t head_n_pages;      /* with head_page_table */
 } glance_packed;
 
 const char *glance_status_string(int32_t status);

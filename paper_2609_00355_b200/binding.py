@@ -57,7 +57,8 @@ class Seqs(C.Structure):
 
 
 class Packed(C.Structure):
-    _fields_ = [("n_pages", C.c_int32), ("len", C.c_void_p), ("page_table", C.c_void_p), ("pool", C.c_void_p)]
+    _fields_ = [("n_pages", C.c_int32), ("len", C.c_void_p), ("page_table", C.c_void_p), ("pool", C.c_void_p),
+                ("head_page_table", C.c_void_p), ("head_n_pages", C.c_int32)]
 
 
 class Tree(C.Structure):
@@ -200,10 +201,11 @@ class PackedCache:
     """Device memory of a 4-bit pool for an engine's target layers, laid out as glance_packed expects.
 
     `n_pages` pages (a layer), as many as the engine's own pool by default, handed out in order; a caller with an allocator of
-    its own writes `page_table` instead.
+    its own writes `page_table` instead.  head_page_table: a page table for the block head's cache, so that the engine's own may
+    give the bf16 pages of packed positions to others.
     """
 
-    def __init__(self, eng: "Engine", n_pages: Optional[int] = None):
+    def __init__(self, eng: "Engine", n_pages: Optional[int] = None, head_page_table: Optional[torch.Tensor] = None):
         self.n_pages = eng.n_pages if n_pages is None else n_pages
         nbytes = eng.lib.glance_packed_bytes(C.byref(eng.ccfg), self.n_pages)
         if nbytes == 0:
@@ -212,7 +214,10 @@ class PackedCache:
         ids = torch.arange(eng.batch * eng.pages_per_seq, dtype=torch.int32, device=eng.device).view(eng.batch, -1)
         self.page_table = torch.where(ids < self.n_pages, ids, -1)
         self.pool = torch.zeros(nbytes, dtype=torch.uint8, device=eng.device)
-        self.c = Packed(self.n_pages, _ptr(self.len), _ptr(self.page_table), _ptr(self.pool))
+        assert head_page_table is None or (head_page_table.dtype is torch.int32 and head_page_table.shape == eng.page_table.shape)
+        self.head_page_table = head_page_table
+        self.c = Packed(self.n_pages, _ptr(self.len), _ptr(self.page_table), _ptr(self.pool), _ptr(head_page_table),
+                        0 if head_page_table is None else eng.n_pages)
 
 
 class Engine:
@@ -474,7 +479,9 @@ class Engine:
         return _gather(self.kv_pool[layer], self.page_table[seq], length, self.cfg.page_size)
 
     def gather_head_kv(self, seq: int, length: int, head_layer: int = 0):
-        return _gather(self.head_kv_all[head_layer], self.page_table[seq], length, self.cfg.page_size)
+        packed = getattr(self, "packed", None)
+        table = self.page_table if packed is None or packed.head_page_table is None else packed.head_page_table
+        return _gather(self.head_kv_all[head_layer], table[seq], length, self.cfg.page_size)
 
 
 def _gather(pool_layer: torch.Tensor, page_table: torch.Tensor, length: int, page: int):

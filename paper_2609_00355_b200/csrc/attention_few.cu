@@ -1068,17 +1068,16 @@ int few_clusters(int S) {
 }
 
 template <int D, int NB, bool TWO>
-cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
+cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, long long pages, cudaStream_t st) {
     using F = Few<D, NB>;
-    static bool once = false;
-    if (!once) {
+    static bool once[kMaxDevices] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (!once[dev]) {
         const cudaError_t e = cudaFuncSetAttribute(attn_few_kernel<D, NB, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::TOTAL);
         if (e != cudaSuccess) return e;
-        once = true;
+        once[dev] = true;
     }
-    // pages that a row can see (the lengths themselves are on the device)
-    long long pages = p.geom.max_pages_per_seq;
-    if (p.window > 0) pages = std::min(pages, ((long long)p.window + p.T + kPage - 1) / kPage + 1 + ((long long)p.sinks + kPage - 1) / kPage);
     const int items = p.Hkv * p.batch;
     // A cluster an item, whose CTAs add their parts through distributed shared memory in 1.5 us, where that costs a CTA no more
     // than kMorePages pages (0.4 us in 4 bits, 0.8 in bf16) beyond its share of the line; there the parts of an item meet in
@@ -1104,14 +1103,16 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStrea
 
 }  // namespace
 
-bool attention_few_takes(int T, int G) { return (long long)T * G <= kFewRows; }
+// (the places of a line are counted in 32 bits)
+bool attention_few_takes(int T, int G, long long items, long long pages) { return (long long)T * G <= kFewRows && (double)items * pages < 1e9; }
 
-cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st) {
+// pages: as many as a row may see (the lengths themselves are on the device)
+cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, long long pages, cudaStream_t st) {
     const int rows = p.T * (p.Hq / p.Hkv);
     auto pick = [&](auto d, auto two) {
         constexpr int D = decltype(d)::value;
         constexpr bool TWO = decltype(two)::value;
-        return rows <= 8 ? launch_few<D, 1, TWO>(p, map_kv, st) : launch_few<D, 2, TWO>(p, map_kv, st);
+        return rows <= 8 ? launch_few<D, 1, TWO>(p, map_kv, pages, st) : launch_few<D, 2, TWO>(p, map_kv, pages, st);
     };
     using D128 = std::integral_constant<int, 128>;
     using D64 = std::integral_constant<int, 64>;

@@ -948,11 +948,13 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
 
 template <int D, int CACHE>
 cudaError_t launch_d(const AttnParams &p, const CUtensorMap &map_kv, dim3 grid, cudaStream_t st) {
-    static bool once = false;
-    if (!once) {
+    static bool once[kMaxDevices] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (!once[dev]) {
         cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, CACHE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
         if (e != cudaSuccess) return e;
-        once = true;
+        once[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;

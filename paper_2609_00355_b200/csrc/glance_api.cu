@@ -309,15 +309,13 @@ void attention_cache(glance_ctx *ctx, AttnParams ap, int layer, int seq_off) {
     ap.parts = ctx->ws.part_rows; ap.parts_ml = ctx->ws.part_ml; ap.part_counters = ctx->ws.part_counters;
     const CUtensorMap *m = get_map(ctx, ap.pool_layer, ap.d, ap.geom.n_pages * 2 * ap.geom.n_kv_heads * kPage, kPage);
     if (!m) return;
-    const bool few = attention_few_takes(ap.T, ap.Hq / ap.Hkv);
-    if (!few) {
-        // pages that a row may see: the lengths themselves are on the device
-        long long pages = c.max_pages_per_seq;
-        if (ap.window > 0) pages = std::min(pages, ((long long)ap.window + ap.T + kPage - 1) / kPage + 1 + ((long long)ap.sinks + kPage - 1) / kPage);
-        attention_cache_splits(ap, pages);
-    }
+    // pages that a row may see: the lengths themselves are on the device
+    long long pages = c.max_pages_per_seq;
+    if (ap.window > 0) pages = std::min(pages, ((long long)ap.window + ap.T + kPage - 1) / kPage + 1 + ((long long)ap.sinks + kPage - 1) / kPage);
+    const bool few = attention_few_takes(ap.T, ap.Hq / ap.Hkv, (long long)ap.batch * ap.Hkv, pages);
+    if (!few) attention_cache_splits(ap, pages);
     const bool prof = prof_begin(ctx);
-    if ((few ? launch_attention_few(ap, *m, ctx->stream) : launch_attention_cache(ap, *m, ctx->stream)) != cudaSuccess) ctx->map_error = true;
+    if ((few ? launch_attention_few(ap, *m, pages, ctx->stream) : launch_attention_cache(ap, *m, ctx->stream)) != cudaSuccess) ctx->map_error = true;
     prof_end(ctx, prof, KIND_ATTN, 0.0);
 }
 
@@ -347,6 +345,16 @@ KvGeom geom_of(const glance_ctx *ctx, const glance_seqs *s) {
     g.head_dim = ctx->cfg.head_dim;
     g.max_pages_per_seq = ctx->cfg.max_pages_per_seq;
     return g;
+}
+
+// the sequences as the block head sees them: its cache may have a page table of its own
+glance_seqs head_view(const glance_ctx *ctx, const glance_seqs *s) {
+    glance_seqs h = *s;
+    if (ctx->held.head_page_table) {
+        h.page_table = ctx->held.head_page_table;
+        h.n_pages = ctx->held.head_n_pages;
+    }
+    return h;
 }
 
 RowMeta meta_of(const glance_ctx *ctx) {
@@ -625,6 +633,8 @@ int32_t glance_prefill(glance_ctx *ctx, const glance_seqs *seqs, int32_t seq, co
         run_target(ctx, ps, ws.hidden_tmp, nullptr, last ? ws.argmax_tmp : nullptr);
         // head context K/V of the new positions (Section 3.2: keys and values are the target's hidden states): every
         // head layer projects the hidden states of the target layer it taps with its own weights into its own pool
+        const glance_seqs hs = head_view(ctx, seqs);
+        const KvGeom hg = geom_of(ctx, &hs);
         for (int i = 0; i < head_depth(c); ++i) {
             const glance_head_layer &hl = ctx->head_layer[i];
             DraftSetup ds{};
@@ -633,13 +643,13 @@ int32_t glance_prefill(glance_ctx *ctx, const glance_seqs *seqs, int32_t seq, co
             ds.feat = ws.hidden_tmp + (size_t)i * n * c.hidden; ds.feat_count = nullptr;
             ds.count_const = n; ds.n_block = 0; ds.embed = ctx->embed; ds.mask_embed = (const bf16 *)ctx->head.mask_embed;
             ds.gain_block = (const bf16 *)hl.ln1; ds.gain_feat = (const bf16 *)hl.ctx_norm;
-            ds.vocab = c.vocab; ds.capacity = c.max_pages_per_seq * kPage; ds.geom = tg; ds.page_table = pt;
+            ds.vocab = c.vocab; ds.capacity = c.max_pages_per_seq * kPage; ds.geom = hg; ds.page_table = hs.page_table + (size_t)seq * c.max_pages_per_seq;
             ds.out = rowout_of(ctx); ds.meta = meta_of(ctx); ds.status = ws.status;
             LAUNCH(ctx, KIND_SETUP, launch_setup_draft(ds, st));
             LayerW hw{(const bf16 *)hl.ln2, (const bf16 *)hl.wqkv, (const bf16 *)hl.wo, (const bf16 *)hl.wgu,
                       (const bf16 *)hl.wd};
-            PassInfo hp{n, 0, 1, n, nullptr, true, seqs, seq};
-            run_layer(ctx, -1, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * tg.layer_stride(), hp, nullptr, nullptr);
+            PassInfo hp{n, 0, 1, n, nullptr, true, &hs, seq};
+            run_layer(ctx, -1, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * hg.layer_stride(), hp, nullptr, nullptr);
         }
         LAUNCH(ctx, KIND_CONTROL, launch_prefill_advance(seqs->seq_len + seq, seqs->root + seq, seqs->feat_count + seq,
                                                          last ? ws.argmax_tmp : nullptr, n, st));
@@ -667,7 +677,8 @@ int32_t glance_draft_block(glance_ctx *ctx, const glance_seqs *seqs, int32_t *to
     cudaStream_t st = ctx->stream;
     const int batch = seqs->batch, B = c.block_B;
     const int R1 = batch * B, R = 2 * R1;
-    const KvGeom hgeom = geom_of(ctx, seqs);
+    const glance_seqs hs = head_view(ctx, seqs);
+    const KvGeom hgeom = geom_of(ctx, &hs);
     const int HL = head_depth(c);
     for (int i = 0; i < HL; ++i) {
         // head layer i: block rows (from the embeddings, or from the layer below) and the feature rows of the
@@ -681,11 +692,11 @@ int32_t glance_draft_block(glance_ctx *ctx, const glance_seqs *seqs, int32_t *to
         ds.embed = ctx->embed; ds.mask_embed = (const bf16 *)ctx->head.mask_embed;
         // block rows use the head layer's input norm, feature rows its context norm
         ds.gain_block = (const bf16 *)hl.ln1; ds.gain_feat = (const bf16 *)hl.ctx_norm; ds.vocab = c.vocab;
-        ds.capacity = c.max_pages_per_seq * kPage; ds.geom = hgeom; ds.page_table = seqs->page_table;
+        ds.capacity = c.max_pages_per_seq * kPage; ds.geom = hgeom; ds.page_table = hs.page_table;
         ds.out = rowout_of(ctx); ds.meta = meta_of(ctx); ds.status = ws.status;
         LAUNCH(ctx, KIND_SETUP, launch_setup_draft(ds, st));
         LayerW hw{(const bf16 *)hl.ln2, (const bf16 *)hl.wqkv, (const bf16 *)hl.wo, (const bf16 *)hl.wgu, (const bf16 *)hl.wd};
-        PassInfo ps{R, R1, batch, B, nullptr, false, seqs, 0};
+        PassInfo ps{R, R1, batch, B, nullptr, false, &hs, 0};
         const bf16 *next_gain = i + 1 < HL ? (const bf16 *)ctx->head_layer[i + 1].ln1 : (const bf16 *)ctx->head.final_norm;
         run_layer(ctx, -1, hw, (bf16 *)seqs->head_kv_pool + (size_t)i * hgeom.layer_stride(), ps, next_gain, nullptr);
     }
@@ -823,6 +834,7 @@ int32_t glance_set_packed(glance_ctx *ctx, const glance_packed *packed) {
         return GLANCE_OK;
     }
     if (packed->n_pages < 1 || !packed->len || !packed->page_table || !packed->pool || ((uintptr_t)packed->pool & 15)) return GLANCE_E_INVALID_ARG;
+    if (packed->head_page_table && packed->head_n_pages < 1) return GLANCE_E_INVALID_ARG;
     ctx->held = *packed;
     return GLANCE_OK;
 }

@@ -157,8 +157,8 @@ struct AttnParams {
 constexpr int kFewRows = 16;
 constexpr int kPartRows = 2 * 148 * kFewRows;        // partial results of a launch: two a CTA, one CTA an SM
 constexpr int kPartCounters = 256;
-bool attention_few_takes(int T, int G);
-cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
+bool attention_few_takes(int T, int G, long long items, long long pages);
+cudaError_t launch_attention_few(const AttnParams &p, const CUtensorMap &map_kv, long long pages, cudaStream_t st);
 // map_kv = 2-D map of the pool layer {d, n_pages*2*Hkv*64 rows}, box {64, 64}
 cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, cudaStream_t st);
 // the same for a cache that is read in part or held in 4 bits (window, sinks, held_*)

@@ -481,6 +481,41 @@ def test_rounds_over_a_packed_cache_replayed_as_a_graph(name, N):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("taps", [(), (0, 1)])
+def test_bf16_pages_of_packed_positions_are_free(taps):
+    """With a page table of its own for the block head, rounds do not look at the target's entries of packed pages: the same bits
+    with those entries gone and their pages overwritten."""
+    from paper_2609_00355_b200.binding import PackedCache
+    cfg = synth.CONFIGS["tiny"].replace(tree_N=8, batch=2, head_taps=taps)
+    logs = [[], []]
+    for which in range(2):
+        eng = seeded_engine(cfg, [150, 200], 24)[0]
+        with torch.cuda.stream(eng.stream):
+            packed = PackedCache(eng, head_page_table=eng.page_table.clone())
+            eng.glance_set_packed(packed)
+            eng.glance_prefill(0, ids=torch.arange(100, dtype=torch.int32, device="cuda"))
+            for _ in range(30):
+                eng.glance_pack_cache(keep=10)
+                if which == 1:
+                    for s, n in enumerate(packed.len.tolist()):
+                        for p in range(n // PAGE):
+                            if int(eng.page_table[s, p]) >= 0:
+                                eng.kv_pool[:, int(eng.page_table[s, p])] = math.nan
+                            eng.page_table[s, p] = -1
+                eng.round()
+                torch.cuda.synchronize()
+                logs[which].append((eng.seq_len.tolist(), packed.len.tolist(), eng.out_tokens.clone(), eng.topk_lp.clone(), eng.hidden_all.clone()))
+            eng.check_device_status()
+            assert packed.len.tolist()[0] >= 192
+            head = [eng.gather_head_kv(s, 100) for s in range(2)]
+            logs[which].append(head)
+    for a, b in zip(logs[0][:-1], logs[1][:-1]):
+        assert a[:2] == b[:2] and all(torch.equal(x, y) for x, y in zip(a[2:], b[2:]))
+    for a, b in zip(logs[0][-1], logs[1][-1]):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.gpu
 def test_truncation_into_the_packed_part():
     """Unpack, truncate, go on: the length held falls with the sequence, and stale 4-bit pages are not read."""
     from paper_2609_00355_b200.binding import PackedCache
