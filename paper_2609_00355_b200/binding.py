@@ -469,10 +469,14 @@ class Engine:
         return g
 
     def snapshot_state(self):
-        return (self.seq_len.clone(), self.root.clone(), self.feat_all.clone(), self.feat_count.clone())
+        snap = (self.seq_len.clone(), self.root.clone(), self.feat_all.clone(), self.feat_count.clone())
+        packed = getattr(self, "packed", None)
+        return snap if packed is None else snap + (packed.len.clone(),)
 
     def restore_state(self, snap):
         self.seq_len.copy_(snap[0]); self.root.copy_(snap[1]); self.feat_all.copy_(snap[2]); self.feat_count.copy_(snap[3])
+        if len(snap) > 4 and getattr(self, "packed", None) is not None:      # a length held in 4 bits falls with its sequence
+            self.packed.len.copy_(torch.minimum(self.packed.len, snap[4]))
 
     def gather_kv(self, seq: int, layer: int, length: int):
         """Logical K,V rows [length, Hkv, d] of one sequence and layer, read back through the page table (tests)."""

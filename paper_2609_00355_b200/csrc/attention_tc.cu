@@ -24,7 +24,7 @@
 // instructions cold, and a CTA of a short context runs this code two or three times.
 // Measured per layer at the 7B widths against 64-key tiles with two threads a row and two S/P buffers a group, us: 128 rows
 // over 8704 positions 72 -> 46, 8 x 64 rows over 1024..4096 97 -> 71, 1280 rows of a prefill 97 -> 42, 64 rows over 1536
-// 17.8 -> 16.2, one row 15 -> 13.3.  What is left of a long loop is the softmax warps (1.85 us per 128-key tile for
+// 17.8 -> 16.2, one row 15 -> 13.3; with the issuing warp going through its loop together the first two 43 and 64.  What is left of a long loop is the softmax warps (1.85 us per 128-key tile for
 // 1.05 of MMAs), of a short one the start and the merge.
 // Warp roles: warp 0 = TMA producer, warp 1 = TMEM allocator + MMA issuer, warps 2..9 = softmax / epilogue.
 // The key splits of a tile form a thread-block cluster and are merged through distributed shared memory
@@ -1031,7 +1031,7 @@ cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, 
 
 // Splits and clusters a tile for a cache that is read in part or held in 4 bits.  As attention_tc_splits; where a launch has few
 // tiles and `pages` (as many as a row may see) leave a CTA more than 12 of them, every tile gets as many clusters of four as fit at
-// once, whose parts meet in global memory (3 to 4 us): 28 rows over 32000 positions 122 us with one cluster of eight a kv head.
+// once, whose parts meet in global memory (3 to 4 us): 28 rows over 32000 positions 122 us with one cluster of eight a kv head, 33 so.
 void attention_cache_splits(AttnParams &p, long long pages) {
     p.S = attention_tc_splits(p.T, p.Hq / p.Hkv, p.Hkv, p.batch, p.d);
     p.clusters = 1;

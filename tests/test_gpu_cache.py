@@ -763,3 +763,30 @@ def test_pools_beyond_four_gigabytes(T):
     run_attention(cache, "tree", 0, 0, 2, hide=False)
     big.glance_unpack_cache(torch.zeros(1, dtype=torch.int32, device="cuda"))
     run_attention(cache, "tree", 0, 0, 2, hide=False)
+
+
+@pytest.mark.gpu
+def test_a_snapshot_takes_the_length_held_in_four_bits_along():
+    """Back to a snapshot, other rows from there on: pages packed in between are not read."""
+    cfg = synth.CONFIGS["tiny"].replace(tree_N=8, batch=1)
+    logs = [[], []]
+    for which in range(2):
+        eng = seeded_engine(cfg, [180], 25, 50)[0]
+        with torch.cuda.stream(eng.stream):
+            snap = eng.snapshot_state()
+            assert len(snap) == 5
+            if which == 1:
+                eng.root.fill_(7)
+                for _ in range(30):
+                    eng.round()
+                eng.glance_pack_cache()
+                assert eng.packed.len.tolist()[0] >= 192
+                eng.restore_state(snap)
+                assert eng.packed.len.tolist() == [128]
+            for _ in range(20):
+                eng.round()
+                torch.cuda.synchronize()
+                logs[which].append((eng.seq_len.clone(), eng.out_tokens.clone(), eng.hidden_all.clone()))
+            eng.check_device_status()
+    for a, b in zip(*logs):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
