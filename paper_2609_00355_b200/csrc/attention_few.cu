@@ -50,13 +50,12 @@ struct Few {
     static constexpr int TEAMS = NB == 1 ? 3 : 2;
     static constexpr int WARPS = TEAMS * kTeam;              // consumers; one more fetches
     static constexpr int THREADS = (WARPS + TEAMS) * 32;
-    // A team has a ring of its own, filled by a warp of its own (a thread that waits, announces and copies takes 270 ns a
-    // page, more than a 4-bit page's share of HBM).  The ring: places of a bf16 page (K and V, multiples of 1024 for the
-    // swizzle), each of which takes three 4-bit tiles in its thirds; a bf16 page goes to a whole place.
+    // A team has a ring of its own, filled by a warp of its own: places of a bf16 page (K and V, multiples of 1024 for the
+    // swizzle) or of three 4-bit tiles in its thirds, the team's next ones.  Three at once, because a thread takes 240 ns to
+    // wait for a place and to announce what it fetches, more than a 4-bit page's share of HBM, and 30 for a copy.
     static constexpr int PAGE_BYTES = 2 * kPage * D * 2;
     static constexpr int THIRD = PAGE_BYTES / 3 / 16 * 16;
     static constexpr int PLACES = 2;                         // a team
-    static constexpr int SLOTS = 3 * PLACES;
     static constexpr int RING = TEAMS * PLACES * PAGE_BYTES;
     static constexpr int ROWF = D + 4;
     static constexpr int QB = 8 * D * 2;                     // one term of 8 rows' queries
@@ -124,9 +123,9 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
                  ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 
-template <int TEAMS, int SLOTS>
+template <int TEAMS, int PLACES>
 struct alignas(8) FewBars {
-    uint64_t full[TEAMS][SLOTS], empty[TEAMS][SLOTS];
+    uint64_t full[TEAMS][PLACES], empty[TEAMS][PLACES];
     int abort_flag, last;
 };
 
@@ -253,13 +252,13 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     unsigned char *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);       // (an offset: the pointer stays a shared one)
     unsigned char *sQ = smem + F::Q_AT;
     float *red = reinterpret_cast<float *>(smem + F::RED_AT);
-    __shared__ FewBars<F::TEAMS, F::SLOTS> bars;
+    __shared__ FewBars<F::TEAMS, F::PLACES> bars;
     __shared__ int upto[kMaxSeqs + 1];                       // pages (of all heads) of the sequences before
     __shared__ int lens[kMaxSeqs], helds[kMaxSeqs];          // positions; pages held in 4 bits
     __shared__ int most_pages[32];                           // of a (sequence, kv head)
     __shared__ float sum_m[8 * NB], sum_l[8 * NB];           // clusters: this CTA's part of its item (the outputs: in `red`)
     __shared__ RowMask mask[8 * NB];
-    __shared__ int pages[F::TEAMS][32];
+    __shared__ int pages[F::TEAMS][64];
     __shared__ float red_m[kWarps][8 * NB], red_l[kWarps][8 * NB];
 
     // test hook: phases of the first CTA (entry, set up, predecessor done, queries staged, first page there, pages done, warps
@@ -274,7 +273,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     volatile int *abort_flag = &bars.abort_flag;
     auto list_of = [&](int P) { return page_list(P + p.T, window_low(P, p.window), p.sinks); };
     if (warp == 0) {
-        for (int i = lane; i < F::TEAMS * F::SLOTS; i += 32) {
+        for (int i = lane; i < F::TEAMS * F::PLACES; i += 32) {
             mbar_init(&bars.full[0][0] + i, 1);
             mbar_init(&bars.empty[0][0] + i, kTeam);
         }
@@ -339,14 +338,17 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     const int team = warp < kWarps ? warp / kTeam : warp - kWarps;
     unsigned char *ring = smem + team * F::PLACES * F::PAGE_BYTES;
     uint64_t *full = bars.full[team], *empty = bars.empty[team];
-    int slot = 0;                                            // of the team's ring: next to be filled or taken, and how often round
+    int place = 0;                                           // of the team's ring: next to be filled or taken, and how often round
     uint32_t phase = 0u;
-    auto advance = [&](int n) {
-        slot += n;
-        if (slot >= F::SLOTS) {
-            slot -= F::SLOTS;
+    auto advance = [&]() {
+        if (++place == F::PLACES) {
+            place = 0;
             phase ^= 1u;
         }
+    };
+    // entries of a stretch [v0, v1) of a list that are held in 4 bits: a prefix
+    auto held_of = [](const PageList &list, int held, int v0, int v1) {
+        return min(max(held <= list.head ? held : list.head + max(held - max(list.next, list.head), 0), v0), v1) - v0;
     };
 
     if (warp >= kWarps) {
@@ -371,55 +373,49 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                 }
                 return page;
             };
-            const int first = v0 + (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS;
-            int ahead = look_up(first + F::TEAMS * lane);
-            int k = 0;                                       // pages of this team in the item
-            for (int v = first; v < v1; v += F::TEAMS, ++k) {
-                if (k % 32 == 0) {
-                    numbers[lane] = ahead;
-                    ahead = look_up(v + F::TEAMS * (32 + lane));
+            const int first = v0 + (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS, v_held = v0 + held_of(list, held, v0, v1);
+            // this team's page k is entry first + TEAMS k; numbers of 64 of them, 32 replaced at a time
+            numbers[lane] = look_up(first + F::TEAMS * lane);
+            numbers[32 + lane] = look_up(first + F::TEAMS * (32 + lane));
+            __syncwarp();
+            int k = 0, upto_k = 64;
+            for (int v = first; v < v1;) {
+                if (k + 32 >= upto_k) {                      // lane 0 is past the older half
+                    __syncwarp();
+                    numbers[(upto_k + lane) & 63] = look_up(first + F::TEAMS * (upto_k + lane));
+                    upto_k += 32;
                     __syncwarp();
                 }
+                const int n = v < v_held ? min(3, (v_held - v + F::TEAMS - 1) / F::TEAMS) : 1;       // pages of this place
                 if (lane == 0 && ok) {
-                    const int pg = list.page(v), page = numbers[k % 32];
-                    if (!waited && (pg + 1) * kPage > P - kMaxBlock) {      // rows that this pass may write
+                    const int last = list.page(v + (n - 1) * F::TEAMS);
+                    if (!waited && (last + 1) * kPage > P - kMaxBlock) {    // rows that this pass may write
                         pdl_wait();
                         waited = true;
                     }
-                    if (pg < held) {
-                        ok = mbar_wait(&empty[slot], phase ^ 1u, abort_flag, p.status);
-                        if (ok) {
-                            mbar_expect_tx(&full[slot], Tile<D>::BYTES);
-                            bulk_load(ring + slot / 3 * F::PAGE_BYTES + slot % 3 * F::THIRD,
-                                      p.held_layer + ((size_t)page * p.Hkv + kvh) * Tile<D>::BYTES, Tile<D>::BYTES, &full[slot]);
-                            advance(1);
-                        }
-                    } else {
-                        while (ok && slot % 3) {             // on to the next place for a whole bf16 page; nothing is put into these
-                            ok = mbar_wait(&empty[slot], phase ^ 1u, abort_flag, p.status);
-                            if (ok) {
-                                mbar_arrive(&full[slot]);
-                                advance(1);
-                            }
-                        }
-                        for (int i = 0; i < 3 && ok; ++i) ok = mbar_wait(&empty[slot + i], phase ^ 1u, abort_flag, p.status);
-                        if (ok) {
-                            mbar_arrive(&full[slot + 1]);
-                            mbar_arrive(&full[slot + 2]);
-                            mbar_expect_tx(&full[slot], F::PAGE_BYTES);
-                            unsigned char *dst = ring + slot / 3 * F::PAGE_BYTES;
+                    ok = mbar_wait(&empty[place], phase ^ 1u, abort_flag, p.status);
+                    if (ok) {
+                        unsigned char *dst = ring + place * F::PAGE_BYTES;
+                        if (v < v_held) {
+                            mbar_expect_tx(&full[place], (uint32_t)(n * Tile<D>::BYTES));
+                            for (int c = 0; c < n; ++c)
+                                bulk_load(dst + c * F::THIRD, p.held_layer + ((size_t)numbers[(k + c) & 63] * p.Hkv + kvh) * Tile<D>::BYTES,
+                                          Tile<D>::BYTES, &full[place]);
+                        } else {
+                            mbar_expect_tx(&full[place], F::PAGE_BYTES);
 #pragma unroll
                             for (int kv = 0; kv < 2; ++kv) {
-                                const int row = ((page * 2 + kv) * p.Hkv + kvh) * kPage;
+                                const int row = ((numbers[k & 63] * 2 + kv) * p.Hkv + kvh) * kPage;
 #pragma unroll
                                 for (int sl = 0; sl < D / 64; ++sl)
-                                    tma_load_2d(dst + (kv * (D / 64) + sl) * (kPage * 128), &map_kv, &full[slot], sl * 64, row);
+                                    tma_load_2d(dst + (kv * (D / 64) + sl) * (kPage * 128), &map_kv, &full[place], sl * 64, row);
                             }
-                            advance(3);
                         }
+                        advance();
                     }
                 }
-                if (k % 32 == 31) __syncwarp();              // the page numbers are no longer read
+                v += n * F::TEAMS;
+                k += n;
             }
             ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
             x += v1 - v0;
@@ -427,10 +423,10 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         if (lane == 0) {
             if (!waited) pdl_wait();
             if (*abort_flag) {                               // copies already issued must land before the CTA may exit
-                for (int i = 0; i < F::SLOTS; ++i) {
-                    // the latest use of slot i: in this round of the ring if it lies before `slot`, else in the last one
+                for (int i = 0; i < F::PLACES; ++i) {
+                    // the latest use of place i: in this round of the ring if it lies before `place`, else in the last one
                     const uint64_t t0 = global_ns();
-                    while (!mbar_try_wait(&full[i], i < slot ? phase : phase ^ 1u))
+                    while (!mbar_try_wait(&full[i], i < place ? phase : phase ^ 1u))
                         if (global_ns() - t0 > kWaitLimitNs) break;
                 }
             }
@@ -607,17 +603,18 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
             }
         };
         // ---------------- pages in 4 bits: a prefix of the stretch's entries ----------------
-        const int n_held = min(max(held <= list.head ? held : list.head + max(held - max(list.next, list.head), 0), v0), v1) - v0;
+        const int n_held = held_of(list, held, v0, v1);
         bool order4 = false;                                 // the accumulators have the 4-bit pages' order of d
         int i = (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS;     // this team's first entry
-        {
-            for (; i < n_held; i += F::TEAMS) {
+        while (i < n_held) {
+            if (!wait_all(&full[place], phase)) break;
+            if (trace && !order4) trace[4] = global_ns();
+            order4 = true;
+            const uint32_t first_tile = ring_addr + (uint32_t)(place * F::PAGE_BYTES);
+#pragma unroll 1
+            for (uint32_t tile = first_tile; tile < first_tile + 3 * F::THIRD && i < n_held; tile += F::THIRD, i += F::TEAMS) {
                 const int pg = list.page(v0 + i), key0 = pg * kPage;
                 const bool open = key0 + kPage <= p.sinks || key0 >= low_max;        // every row sees all of it (it lies below P)
-                if (!wait_all(&full[slot], phase)) break;
-                if (trace && !order4) trace[4] = global_ns();
-                order4 = true;
-                const uint32_t tile = ring_addr + (uint32_t)(slot / 3 * F::PAGE_BYTES + slot % 3 * F::THIRD);
                 float cc[CH][NB][4];
                 {
                     constexpr int WORDS = D / 32;            // words of a key that a lane takes: d = (D/4) t ..
@@ -719,19 +716,13 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                         }
                     }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&empty[slot]);
-                advance(1);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty[place]);
+            advance();
         }
         // ---------------- pages in bf16 ----------------
         if (ok && i < v1 - v0) {
-            while (ok && slot % 3) {                         // the producer's way to the next whole place
-                if (wait_all(&full[slot], phase)) {
-                    if (lane == 0) mbar_arrive(&empty[slot]);
-                    advance(1);
-                }
-            }
             if (order4) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) reorder<D>(O[nb], g);
@@ -740,9 +731,9 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
             for (; i < v1 - v0; i += F::TEAMS) {
                 const int pg = list.page(v0 + i), key0 = pg * kPage;
                 const bool open = key0 + kPage <= P && (key0 + kPage <= p.sinks || key0 >= low_max);     // every row sees all of it
-                if (!wait_all(&full[slot], phase)) break;
+                if (!wait_all(&full[place], phase)) break;
                 if (trace && n_held == 0 && i < F::TEAMS) trace[4] = global_ns();
-                const uint32_t kbase = smem_u32(ring + slot / 3 * F::PAGE_BYTES), vbase = kbase + kPage * D * 2;
+                const uint32_t kbase = smem_u32(ring + place * F::PAGE_BYTES), vbase = kbase + kPage * D * 2;
                 float cc[CH][NB][4];
                 // lane's row of the four 8 x 8 matrices it addresses
                 const int mi = lane >> 3, r = first_key + key_of(lane & 7);
@@ -794,8 +785,8 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                     }
                 }
                 __syncwarp();
-                if (lane < 3) mbar_arrive(&empty[slot + lane]);
-                advance(3);
+                if (lane == 0) mbar_arrive(&empty[place]);
+                advance();
             }
         }
 
