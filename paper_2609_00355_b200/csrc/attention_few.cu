@@ -2,8 +2,8 @@
 // window, sinks) or held in 4 bits: bound by the bytes of the cache, so everything is laid out around streaming them once.
 //
 // The pages that a launch has to read form one line: sequences, in each its kv heads, in each the pages that some row sees
-// (packed.cuh).  The line is dealt out in equal stretches to one CTA an SM, so ragged batches and long single sequences
-// keep the whole GPU reading; a CTA finds its stretch from the device-resident lengths by one prefix sum.  Teams of four warps
+// (packed.cuh).  The line is dealt out in stretches of equal cost to one CTA an SM, so ragged batches and long single
+// sequences keep the whole GPU reading; a CTA finds its stretch from the device-resident lengths by one prefix sum.  Teams of four warps
 // take its pages in turn, a warp 16 of a page's 64 keys, and nobody waits for another inside an item; a team's producer warp
 // fetches its pages into its ring (bf16: tensor copies; 4 bits: one bulk copy of a 4.5-bit tile).
 //     S^T[16 keys x 8 rows] = K Q^T,   O^T[d x 8 rows] += V^T P^T     (mma.sync m16n8k16, fp32 accumulators)
@@ -17,9 +17,11 @@
 // A row's reference is raised only when a score exceeds the largest so far by 2^8; sums and accumulators are fp32.
 // The warps' partial results meet in shared memory; an item that several CTAs share is finished by the one that comes last,
 // which adds the parts in line order, or by its cluster through distributed shared memory: results do not depend on timing.
-// Measured (us): 16 rows of 7 heads over 4096-32768 positions in 4 bits, 160 MB, 52 (3.1 TB/s: the conversions, ALU pipe at 46 %
-// of a rate of one instruction in two clocks, issue slots 58 %); over 8192 positions in bf16, 269 MB, 47 (5.5 TB/s); one row
-// over 32801 positions in 4 bits 14.6, of which 5.5 are the merge of 37 parts; one row over a window of 512 7.5.
+// Measured (us): 16 rows of 7 heads over 4096-32768 positions in 4 bits, 160 MB, 44.9 (3.6 TB/s); over 8192 positions in bf16,
+// 262 MB, 50.2 (5.2 TB/s); one row over 32801 positions in 4 bits 14.9, of which 5.5 are the merge of 37 parts; one row over a
+// window of 512 7.0.  In 4 bits the bound is the chain of a page in its warp (1300 clocks: first products 450, softmax 200,
+// second products 620), of which 12 warps keep three pages going; variants without the conversions, without the products of one
+// side or with twice the loads ahead ended within 5 % of it.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,7 +41,7 @@ constexpr int kMaxSeqs = 64;
 constexpr float kRaise = 8.f;                // log2 units a score may exceed its reference by
 constexpr float kHead = 7.f;                 // and the reference lies this far below the largest: fp16 probabilities reach from 2^15 down
                                              // to 2^-14 at full precision, 2^-21 of the largest
-constexpr int kEven = 6;                     // pages a CTA may have more to have one item only (see the kernel)
+constexpr int kLead4 = 24, kLead16 = 4;      // pages, in 4 bits and in bf16, that an item's end and the next one's start are worth (see the kernel)
 constexpr int kMaxCluster = 8;
 constexpr int kMorePages = 3;                // pages a CTA may have more to be in a cluster (see launch_few)
 
@@ -311,28 +313,64 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         if (lane == 0) upto[0] = 0;
     }
     __syncthreads();
-    // ---- this CTA's stretch of the line: with clusters, a share of its cluster's item ((sequence, kv head)); else either equal
-    // stretches, which may begin and end inside an item, or, where that costs the longest item no more than kEven pages, the
-    // same number of CTAs for every item, so that a CTA has one item to start and to finish (4 to 5 us each) ----
-    const int total = upto[p.batch], items = p.batch * p.Hkv;
-    int most = most_pages[lane];
+    // ---- this CTA's stretch of the line: with clusters, a share of its cluster's item ((sequence, kv head)).  Else the same number of
+    // CTAs for every item, so that a CTA has one item to start and to finish, unless equal stretches, which may begin and end
+    // inside an item, end earlier.  To finish an item and start the next takes a CTA as long as `lead` pages, so on the line every
+    // item begins with that many places without a page (16 rows over 4096-32768 positions in 4 bits: without them CTAs with
+    // one item ended after 37 us, those with two after 47; whole launch 49.4; with 24 places 44.9, 16 and 32 1.3 and 0.4 more) ----
+    int chunk, lead = 0, s, kvh, pos, places;                // the first item's place to begin with (lead first); places of the stretch
+    {
+        const int items = p.batch * p.Hkv, grid = (int)gridDim.x, total = upto[p.batch];
+        int per_item = p.S;
+        if (p.S == 0) {
+            int most = most_pages[lane];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
-    int chunk = (total + (int)gridDim.x - 1) / (int)gridDim.x, per_item = p.S > 0 ? p.S : (int)gridDim.x / items;
-    if (p.S == 0 && per_item > 0 && (most + per_item - 1) / per_item > chunk + kEven) per_item = 0;
-    int s = 0, x_begin, x_end;
-    if (per_item > 0) {
-        const int item = (int)blockIdx.x / per_item, sub = (int)blockIdx.x % per_item;
-        s = min(item / p.Hkv, p.batch - 1);
-        const int n = (upto[s + 1] - upto[s]) / p.Hkv, first = upto[s] + item % p.Hkv * n;
-        chunk = (n + per_item - 1) / per_item;
-        x_begin = first + min(sub * chunk, n);
-        x_end = item < items ? first + min((sub + 1) * chunk, n) : x_begin;
-    } else {
-        x_begin = min((int)blockIdx.x * chunk, total);
-        x_end = min(x_begin + chunk, total);
-        while (s + 1 < p.batch && upto[s + 1] <= x_begin) ++s;
+            for (int o = 16; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+            per_item = grid / items;
+            lead = min(p.held_len ? kLead4 : kLead16, (total + grid - 1) / grid / 2);
+            if (per_item > 0 && (most + per_item - 1) / per_item <= (total + lead * items + grid - 1) / grid) lead = 0;
+            else per_item = 0;
+        }
+        if (per_item > 0) {
+            const int item = (int)blockIdx.x / per_item;
+            s = min(item / p.Hkv, p.batch - 1);
+            kvh = item - s * p.Hkv;
+            const int n = list_of(lens[s]).count;
+            chunk = (n + per_item - 1) / per_item;
+            pos = ((int)blockIdx.x - item * per_item) * chunk;
+            places = item < items ? min(chunk, n - pos) : 0;
+        } else {
+            const int line = total + items * lead;
+            chunk = (line + grid - 1) / grid;
+            const int x = (int)blockIdx.x * chunk;
+            places = min(chunk, line - x);
+            s = 0;
+            while (s + 1 < p.batch && upto[s + 1] + (s + 1) * p.Hkv * lead <= x) ++s;
+            const int n = list_of(lens[s]).count + lead;
+            pos = x - upto[s] - s * p.Hkv * lead;
+            kvh = pos / n;
+            pos -= kvh * n;
+        }
     }
+    // the part of item (s, kvh) from pos on that lies in the stretch, of which `at` places are behind: entries [v0, v1) of its
+    // list; and on to the next item, or the end of the stretch
+    struct Part {
+        int v0, v1, from;                                    // from: place of the item's first page, counted from the stretch's begin
+    };
+    int at = 0;
+    auto next_part = [&](int count) {
+        const int end = min(count + lead, pos + places - at);
+        const Part part{max(pos - lead, 0), max(end - lead, 0), at + lead - pos};
+        at += end - pos;
+        return part;
+    };
+    auto next_item = [&]() {
+        pos = 0;
+        if (++kvh == p.Hkv) {
+            kvh = 0;
+            ++s;
+        }
+    };
 
     // Page i of the CTA's stretch belongs to team i % TEAMS.
     const int team = warp < kWarps ? warp / kTeam : warp - kWarps;
@@ -355,12 +393,13 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         // ---------------- a team's producer: lane 0 issues; all lanes look up page numbers, 32 at a time and ahead ----------------
         bool waited = false, ok = true;
         int *numbers = pages[team];
-        for (int x = x_begin; x < x_end && ok;) {
-            while (upto[s + 1] <= x) ++s;
+        int done = 0;                                        // pages of the stretch so far
+        for (; at < places && ok; next_item()) {
             const int P = lens[s], held = helds[s];
             const PageList list = list_of(P);
-            const int kvh = (x - upto[s]) / list.count, v0 = (x - upto[s]) % list.count;
-            const int v1 = min(list.count, v0 + (x_end - x));
+            const Part part = next_part(list.count);
+            const int v0 = part.v0, v1 = part.v1;
+            if (v0 == v1) continue;
             auto look_up = [&](int v) {                      // page of entry v in its pool
                 if (v >= v1) return 0;
                 const int pg = list.page(v);
@@ -373,7 +412,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                 }
                 return page;
             };
-            const int first = v0 + (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS, v_held = v0 + held_of(list, held, v0, v1);
+            const int first = v0 + (team + F::TEAMS - done % F::TEAMS) % F::TEAMS, v_held = v0 + held_of(list, held, v0, v1);
             // this team's page k is entry first + TEAMS k; numbers of 64 of them, 32 replaced at a time
             numbers[lane] = look_up(first + F::TEAMS * lane);
             numbers[32 + lane] = look_up(first + F::TEAMS * (32 + lane));
@@ -418,7 +457,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                 k += n;
             }
             ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-            x += v1 - v0;
+            done += v1 - v0;
         }
         if (lane == 0) {
             if (!waited) pdl_wait();
@@ -467,18 +506,19 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     const uint32_t at_vs1 = Tile<D>::HALF + Tile<D>::SCALES + kV1 * Tile<D>::GROUPS + (D == 128 ? g : g >> 1);
 
     // (a warp whose wait gave up takes no more pages, but goes through every barrier and counts its items in)
-    for (int x = x_begin; x < x_end;) {
-        while (upto[s + 1] <= x) ++s;
+    int done = 0;                                            // pages of the stretch so far
+    for (; at < places; next_item()) {
         const int P = lens[s], held = helds[s];
         const PageList list = list_of(P);
-        const int kvh = (x - upto[s]) / list.count, v0 = (x - upto[s]) % list.count;
-        const int v1 = min(list.count, v0 + (x_end - x));
+        const Part part = next_part(list.count);
+        const int v0 = part.v0, v1 = part.v1;
+        if (v0 == v1) continue;
         const int n_keys = P + p.T;
         const int low_min = window_low(P, p.window);         // some row may see positions from here on
         const int low_max = p.window > 0 ? window_low(P + p.T - 1, p.window) : low_min;       // every row does
 
         // ---- the item's queries and what they see ----
-        if (x > x_begin) asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");      // the previous item's are no longer read
+        if (done > 0) asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");      // the previous item's are no longer read
         for (int r = tid - (kWarps - 1) * 32; r >= 0 && r < 8 * NB; r += 32) {
             RowMask rm;
             rm.low = 0x7fffffff;                             // rows that do not exist see nothing
@@ -605,7 +645,8 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         // ---------------- pages in 4 bits: a prefix of the stretch's entries ----------------
         const int n_held = held_of(list, held, v0, v1);
         bool order4 = false;                                 // the accumulators have the 4-bit pages' order of d
-        int i = (team + F::TEAMS - (x - x_begin) % F::TEAMS) % F::TEAMS;     // this team's first entry
+        int i = (team + F::TEAMS - done % F::TEAMS) % F::TEAMS;              // this team's first entry
+        done += v1 - v0;
         while (i < n_held) {
             if (!wait_all(&full[place], phase)) break;
             if (trace && !order4) trace[4] = global_ns();
@@ -792,11 +833,11 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
 
         if (trace) trace[5] = global_ns();
         // ---- the warps' parts meet; this CTA's part of the item, or all of it ----
-        const int item = s * p.Hkv + kvh;
-        const int first_x = x - v0, last_x = first_x + list.count - 1;       // the item's places in the line
-        const int c_first = per_item > 0 ? (s * p.Hkv + kvh) * per_item : first_x / chunk;
-        const int parts = per_item > 0 ? (list.count + chunk - 1) / chunk : last_x / chunk - c_first + 1;
-        const int part = 2 * (int)blockIdx.x + (first_x > x_begin ? 1 : 0);  // a CTA shares its first item, its last, or both
+        // the item's first page lies in the stretch of CTA blockIdx - back; the item spreads over `parts` stretches
+        const int back = part.from < 0 ? (chunk - 1 - part.from) / chunk : 0;
+        const int parts = (part.from + back * chunk + list.count - 1) / chunk + 1;
+        // a CTA may share an item that began before its stretch (its first part), and the one that begins in it last (its second)
+        const int slot = 2 * (int)blockIdx.x + (part.from >= 0 ? 1 : 0);
         const int rows = min(PR, 8 * NB);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -858,12 +899,12 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                 const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
                 store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
             } else {
-                *reinterpret_cast<float4 *>(p.parts + ((size_t)part * kFewRows + row) * D + d0) = acc;
-                if (d0 == 0) reinterpret_cast<float2 *>(p.parts_ml)[(size_t)part * kFewRows + row] = make_float2(M, L);
+                *reinterpret_cast<float4 *>(p.parts + ((size_t)slot * kFewRows + row) * D + d0) = acc;
+                if (d0 == 0) reinterpret_cast<float2 *>(p.parts_ml)[(size_t)slot * kFewRows + row] = make_float2(M, L);
             }
         };
         constexpr int ELEMS = 8 * (D / 4), WARP_F = 8 * F::ROWF;             // of 8 rows
-        if (x + (v1 - v0) == x_end) {
+        if (places - at <= lead) {
             // The CTA's last item: no more pages come, so the rings hold the accumulators of all warps and blocks at once.
             asm volatile("bar.sync %0, %1;" ::"r"(2 + team), "n"(kTeam * 32) : "memory");        // the team has read its last page
             float *mine = reinterpret_cast<float *>(ring);
@@ -916,16 +957,15 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                 // releases what the whole CTA wrote (the barrier orders it before this thread), acquires the others' parts
                 int before;
                 __threadfence();
-                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.part_counters + item) : "memory");
+                asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.part_counters + s * p.Hkv + kvh) : "memory");
                 bars.last = before == parts - 1;
-                if (bars.last) p.part_counters[item] = 0;    // for the next launch
+                if (bars.last) p.part_counters[s * p.Hkv + kvh] = 0;    // for the next launch
             }
             asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
             if (trace) trace[7] = global_ns();
             if (bars.last) {
                 // every team takes every TEAMS-th part, 8 elements a thread; the teams' sums meet in shared memory
-                // (the part of the item's first CTA is its second one if another item came before)
-                const int s_first = 2 * c_first + (per_item == 0 && first_x > c_first * chunk ? 1 : 0);
+                const int c_first = (int)blockIdx.x - back;
                 float *team_m = &red_m[0][0], *team_l = &red_l[0][0];        // [team][8 NB]
                 for (int i = tid % (kTeam * 32); i < rows * (D / 8); i += kTeam * 32) {
                     const int row = i / (D / 8), d0 = i % (D / 8) * 8;
@@ -940,10 +980,10 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
 #pragma unroll
                         for (int k = 0; k < U; ++k) {
                             const int c = min(c0 + k * F::TEAMS, parts - 1);
-                            const size_t at = (size_t)(c == 0 ? s_first : 2 * (c_first + c)) * kFewRows + row;
-                            ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.parts_ml) + at);
-                            a[k][0] = __ldcg(reinterpret_cast<const float4 *>(p.parts + at * D + d0));
-                            a[k][1] = __ldcg(reinterpret_cast<const float4 *>(p.parts + at * D + d0) + 1);
+                            const size_t slot = (size_t)(2 * (c_first + c) + (c == 0 ? 1 : 0)) * kFewRows + row;
+                            ml[k] = __ldcg(reinterpret_cast<const float2 *>(p.parts_ml) + slot);
+                            a[k][0] = __ldcg(reinterpret_cast<const float4 *>(p.parts + slot * D + d0));
+                            a[k][1] = __ldcg(reinterpret_cast<const float4 *>(p.parts + slot * D + d0) + 1);
                         }
                         float M2 = M;
 #pragma unroll
@@ -992,7 +1032,6 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                 }
             }
         }
-        x += v1 - v0;
     }
     if (p.S > 0) {
         // ---- the cluster's CTAs hold a part of one item each: every CTA adds its share of the elements over all of them ----
