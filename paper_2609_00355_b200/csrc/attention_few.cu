@@ -20,8 +20,8 @@
 // Measured (us): 16 rows of 7 heads over 4096-32768 positions in 4 bits, 160 MB, 44.9 (3.6 TB/s); over 8192 positions in bf16,
 // 262 MB, 50.2 (5.2 TB/s); one row over 32801 positions in 4 bits 14.9, of which 5.5 are the merge of 37 parts; one row over a
 // window of 512 7.0.  In 4 bits the bound is the chain of a page in its warp (1300 clocks: first products 450, softmax 200,
-// second products 620), of which 12 warps keep three pages going; variants without the conversions, without the products of one
-// side or with twice the loads ahead ended within 5 % of it.
+// second products 620), of which 12 warps keep three pages going; variants without the conversions, the mma or V's products
+// saved next to nothing.
 #include <algorithm>
 #include <type_traits>
 
