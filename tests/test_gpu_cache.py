@@ -711,6 +711,16 @@ def test_stretches_of_a_batch(heads, lens, window, sinks, held):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("held", [None, 64])
+@pytest.mark.parametrize("heads,n", [(H7, 23), ((32, 8, 128), 13), ((16, 1, 64), 61)])
+def test_stretches_that_end_between_items(heads, n, held):
+    """Many items of very different lengths: a CTA takes short ones whole, and stretches begin and end before an item's first page."""
+    cache = Cache(heads, [(i * i * 131) % 4001 for i in range(n)], 1, 53, held=held)
+    run_attention(cache, "block", 0, 0, 8)
+    run_attention(cache, "block", 0, 0, 9, two=True, hide=False)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("heads,T", [(H7, 2), (H7, 40), (HS, 3), (HS, 70)])
 def test_rows_that_see_nothing_are_zeros(heads, T):
     """Empty sets over no context, in one call with rows that see something; and sets without the row itself."""
