@@ -475,8 +475,12 @@ class Engine:
 
     def restore_state(self, snap):
         self.seq_len.copy_(snap[0]); self.root.copy_(snap[1]); self.feat_all.copy_(snap[2]); self.feat_count.copy_(snap[3])
-        if len(snap) > 4 and getattr(self, "packed", None) is not None:      # a length held in 4 bits falls with its sequence
-            self.packed.len.copy_(torch.minimum(self.packed.len, snap[4]))
+        packed = getattr(self, "packed", None)
+        if packed is not None:
+            # A length held in 4 bits falls with its sequence, whether or not the snapshot knows of a pool: pages packed
+            # since hold rows that the sequence will write anew.
+            held = torch.minimum(packed.len, self.seq_len // self.cfg.page_size * self.cfg.page_size)
+            packed.len.copy_(torch.minimum(held, snap[4]) if len(snap) > 4 else held)
 
     def gather_kv(self, seq: int, layer: int, length: int):
         """Logical K,V rows [length, Hkv, d] of one sequence and layer, read back through the page table (tests)."""

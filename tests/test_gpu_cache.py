@@ -800,3 +800,55 @@ def test_a_snapshot_takes_the_length_held_in_four_bits_along():
             eng.check_device_status()
     for a, b in zip(*logs):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_a_snapshot_from_before_the_pool_bounds_the_length_held():
+    """restore_state on host tensors: whole pages of the restored length are the most that stays held in 4 bits."""
+    from types import SimpleNamespace
+
+    from paper_2609_00355_b200.binding import Engine
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)
+    eng = SimpleNamespace(cfg=SimpleNamespace(page_size=PAGE), seq_len=i32(180, 700, 63, 640), root=i32(1, 2, 3, 4),
+                          feat_all=torch.zeros(1, 4, 2, 8), feat_count=i32(0, 0, 0, 0))
+    snap = Engine.snapshot_state(eng)
+    assert len(snap) == 4
+    eng.packed = SimpleNamespace(len=i32(256, 640, 64, 640))
+    later = Engine.snapshot_state(eng)
+    eng.seq_len.add_(200)
+    Engine.restore_state(eng, snap)
+    assert eng.seq_len.tolist() == [180, 700, 63, 640]
+    assert eng.packed.len.tolist() == [128, 640, 0, 640]
+    eng.packed.len.copy_(i32(320, 832, 128, 768))
+    Engine.restore_state(eng, later)
+    assert eng.packed.len.tolist() == [128, 640, 0, 640]
+
+
+@pytest.mark.gpu
+def test_back_to_a_snapshot_from_before_the_pool():
+    """Snapshot, register a pool, run and pack, go back, run on: rows written since are not read from 4-bit pages.  The same
+    bits as an engine that packed at the snapshot's length."""
+    from paper_2609_00355_b200.binding import PackedCache
+    cfg = synth.CONFIGS["tiny"].replace(tree_N=8, batch=1)
+    logs = [[], []]
+    for which in range(2):
+        eng = seeded_engine(cfg, [180], 25)[0]
+        with torch.cuda.stream(eng.stream):
+            snap = eng.snapshot_state()
+            eng.glance_set_packed(PackedCache(eng))
+            if which == 1:
+                eng.root.fill_(7)
+                for _ in range(30):
+                    eng.round()
+                eng.glance_pack_cache()
+                assert eng.packed.len.tolist()[0] >= 192
+                eng.restore_state(snap)
+            else:
+                eng.glance_pack_cache()
+            assert eng.packed.len.tolist() == [128]
+            for _ in range(30):
+                eng.round()
+                torch.cuda.synchronize()
+                logs[which].append((eng.seq_len.clone(), eng.out_tokens.clone(), eng.hidden_all.clone()))
+            eng.check_device_status()
+    for a, b in zip(*logs):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
