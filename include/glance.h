@@ -234,14 +234,17 @@ size_t glance_packed_bytes(const glance_config *cfg, int32_t n_pages);
 int32_t glance_set_packed(glance_ctx *ctx, const glance_packed *packed);
 
 /* Moves finished pages of every sequence and target layer from kv_pool into the registered 4-bit pool: len[s] rises to
- * max(0, seq_len[s] - keep) rounded down to whole pages (and never falls here).  keep >= 0 positions at least stay in bf16.
- * The bf16 pages are left as they are.  kv_pool has to be 32-byte aligned here and in glance_unpack_cache.  GLANCE_E_STATE
- * without a registered pool. */
+ * max(0, seq_len[s] - keep) rounded down to whole pages (and falls only to whole pages of seq_len[s], where it was above them).
+ * keep >= 0 positions at least stay in bf16.  The bf16 pages are left as they are.  Where a page due has no place, its entry in
+ * either page table being outside its pool, len[s] rises as far as that page and the status word says GLANCE_E_BOUNDS: a
+ * sequence whose pages of the 4-bit pool are used up stays in bf16 from there on, and its other pages and the other sequences'
+ * move all the same.  kv_pool has to be 32-byte aligned here and in glance_unpack_cache.  GLANCE_E_STATE without a registered pool. */
 int32_t glance_pack_cache(glance_ctx *ctx, const glance_seqs *seqs, int32_t keep);
 
 /* The way back: len[s] falls to new_len[s] rounded down to whole pages (device [batch]; larger values change nothing), and
- * the values that the pages from there on stand for are written to the pages of seqs->kv_pool.  Before a truncation into the
- * 4-bit part, or to look at what is held (with a kv_pool of the caller's own in *seqs).  GLANCE_E_STATE without a pool. */
+ * the values that the pages from there on stand for are written to the pages of seqs->kv_pool.  Where a page due has no place
+ * (as above), len[s] falls only to behind the last such page, with GLANCE_E_BOUNDS in the status word.  Before a truncation into
+ * the 4-bit part, or to look at what is held (with a kv_pool of the caller's own in *seqs).  GLANCE_E_STATE without a pool. */
 int32_t glance_unpack_cache(glance_ctx *ctx, const glance_seqs *seqs, const int32_t *new_len);
 
 /* The attention of a target layer's pass over the paged cache, by itself: T rows of each sequence, q (device [batch*T][Hq*d]

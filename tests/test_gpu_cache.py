@@ -852,3 +852,78 @@ def test_back_to_a_snapshot_from_before_the_pool():
             eng.check_device_status()
     for a, b in zip(*logs):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,layers", [(H7, 2), (HS, 3)])
+def test_packing_stops_before_a_page_without_a_place(heads, layers):
+    """A pool with fewer pages than the sequences: the lengths rise as far as there are places, pages that have one move, the
+    call reports it, and attention over what is there is right; with the places given, the rest follows."""
+    from paper_2609_00355_b200.binding import PackedCache
+    lens, T = [700, 300, 130, 1000], 2
+    cache = Cache(heads, lens, T, 91, layers=layers)
+    eng, x = cache.eng, cache.eng.kv_pool.clone()
+    packed = PackedCache(eng)
+    table, own = eng.page_table.clone(), packed.page_table.clone()
+    packed.page_table[0, 6] = -1                         # sequence 0 ends in the pool after six pages
+    packed.page_table[0, 8] = packed.n_pages
+    packed.page_table[1, 4] = -5                         # not due: 300 positions are four pages
+    packed.page_table[3, 0] = packed.n_pages + 3         # sequence 3 finds none at all
+    eng.page_table[2, 1] = eng.n_pages                   # and a page that is not in the bf16 pool cannot move either
+    eng.glance_set_packed(packed)
+    eng.glance_pack_cache()
+    assert eng.glance_poll_status() == -6
+    assert packed.len.tolist() == [6 * 64, 4 * 64, 64, 0]
+    assert torch.equal(torch.nan_to_num(eng.kv_pool), torch.nan_to_num(x))
+    eng.glance_pack_cache()                              # it stays so
+    assert eng.glance_poll_status() == -6
+    assert packed.len.tolist() == [6 * 64, 4 * 64, 64, 0]
+    eng.page_table.copy_(table)
+    K, V = [k.clone() for k in cache.K], [v.clone() for v in cache.V]
+
+    def compare():
+        for s, n in enumerate(packed.len.tolist()):
+            cache.K[s], cache.V[s] = K[s].clone(), V[s].clone()
+            cache.K[s][:n], cache.V[s][:n] = held_values(K[s][:n]), held_values(V[s][:n])
+        run_attention(cache, "block", 0, 0, 1, hide=False)
+        run_attention(cache, "block", 200, 70, 1, hide=False)
+    compare()
+    packed.page_table.copy_(own)
+    eng.glance_pack_cache()
+    eng.check_device_status()
+    assert packed.len.tolist() == [P // 64 * 64 for P in lens]
+    compare()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,layers", [(H7, 2), (HS, 3)])
+def test_unpacking_stops_behind_a_page_without_a_place(heads, layers):
+    """The way back: a length does not fall below a page that could not be written, and the pages behind it are."""
+    from paper_2609_00355_b200.binding import PackedCache
+    lens, T = [700, 300, 130, 1000], 2
+    cache = Cache(heads, lens, T, 92, layers=layers)
+    eng, x = cache.eng, cache.eng.kv_pool.clone()
+    packed = PackedCache(eng)
+    eng.glance_set_packed(packed)
+    eng.glance_pack_cache()
+    eng.check_device_status()
+    K, V = [k.clone() for k in cache.K], [v.clone() for v in cache.V]
+    table, own = eng.page_table.clone(), packed.page_table.clone()
+    eng.page_table[0, 2] = -1                            # due from page 1 on: pages 6.. come back
+    eng.page_table[0, 5] = eng.n_pages
+    eng.page_table[1, 0] = -1                            # not due
+    packed.page_table[3, 14] = -1                        # the last one held has no place to be read from: nothing comes back
+    back = torch.full_like(x, 3.0)
+    eng.glance_unpack_cache(torch.tensor([64, 128, 1 << 20, 0], dtype=torch.int32, device="cuda"), kv_pool=back)
+    assert eng.glance_poll_status() == -6
+    assert packed.len.tolist() == [6 * 64, 128, 128, 15 * 64]
+    ref = torch.full(x.shape, 3.0, dtype=torch.float64, device="cuda")
+    for s, pages in ((0, range(6, 10)), (1, (2, 3))):
+        for p in pages:
+            ref[:, int(table[s, p])] = held_values(x[:, int(table[s, p])])
+    assert torch.equal(back.double(), ref)
+    packed.page_table.copy_(own)
+    for s, n in enumerate(packed.len.tolist()):
+        cache.K[s][:n], cache.V[s][:n] = held_values(K[s][:n]), held_values(V[s][:n])
+    eng.page_table[0, :6] = -1                           # what is held is read from where it is held
+    run_attention(cache, "block", 0, 0, 1, hide=False)
