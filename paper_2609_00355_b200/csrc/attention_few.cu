@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
     }
     if (threadIdx.x < 8 * NB) {
         sum_m[threadIdx.x] = -INFINITY;
-        sum_l[threadIdx.x] = 0.f;
+        sum_l[threadIdx.x] = -1.f;                           // no pages yet
     }
     if (!p.early) pdl_wait();
     if (warp == 1) {
@@ -1055,10 +1055,11 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
 #pragma unroll
             for (int k = 0; k < kMaxCluster; ++k)
                 if (k < p.S) M = fmaxf(M, pm[k]);
+            if (M == -INFINITY) M = 0.f;
 #pragma unroll
             for (int k = 0; k < kMaxCluster; ++k)
-                if (k < p.S && pm[k] != -INFINITY) {         // (a CTA without pages wrote no outputs)
-                    const float f = ex2(pm[k] - M);
+                if (k < p.S && !(pl[k] < 0.f)) {             // (a CTA without pages wrote no outputs)
+                    const float f = ex2(pm[k] - M);          // 2^-inf = 0 for a part without a maximum: NaN where the row's scores were
                     L += f * pl[k];
                     acc.x += f * a[k].x; acc.y += f * a[k].y; acc.z += f * a[k].z; acc.w += f * a[k].w;
                 }

@@ -927,3 +927,38 @@ def test_unpacking_stops_behind_a_page_without_a_place(heads, layers):
         cache.K[s][:n], cache.V[s][:n] = held_values(K[s][:n]), held_values(V[s][:n])
     eng.page_table[0, :6] = -1                           # what is held is read from where it is held
     run_attention(cache, "block", 0, 0, 1, hide=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS])
+@pytest.mark.parametrize("two", [False, True])
+@pytest.mark.parametrize("kind,T,lens,window,sinks,held", [
+    ("block", 1, [1536], 512, 4, None), ("block", 1, [1536], 512, 4, 64), ("block", 1, [40, 64, 700], 100, 0, 64), ("block", 2, [0, 300], 0, 0, 64),
+    ("block", 1, [9000], 0, 0, 64), ("block", 1, [500, 6000, 100], 0, 0, 64), ("tree", 64, [1536], 512, 4, None), ("tree", 40, [700, 64], 0, 0, 64),
+    ("tree", 8, [9000], 0, 0, 64), ("chain", 200, [300], 100, 5, None)])
+def test_a_nan_in_a_query_stays_in_its_row(heads, two, kind, T, lens, window, sinks, held):
+    """Whatever plan a launch has: every output of a query with a NaN is NaN, and the other rows keep their bits."""
+    cache = Cache(heads, lens, T, 81, held=held)
+    eng, (Hq, Hkv, d) = cache.eng, heads
+    rng = np.random.default_rng(1)
+    anc = torch.from_numpy(np.stack([anc_words(np.arange(T) - 1) for _ in lens])).cuda() if kind == "tree" else None
+    n = len(lens) * T
+    call = lambda q, q_lo, out, lo: eng.glance_attention(0, q, T, out, anc=anc, causal=kind == "chain", window=window, sinks=sinks, q_lo=q_lo, out_lo=lo)
+    lo_in = (cache.q * 2.0 ** -9).contiguous() if two else None
+    outs = []
+    bad = sorted({(int(rng.integers(0, n)), int(rng.integers(0, Hq))) for _ in range(3)})
+    q = cache.q.clone()
+    for r, h in bad:
+        q[r, h * d + int(rng.integers(0, d))] = math.nan
+    for x in (cache.q, q):
+        out = torch.zeros_like(x)
+        lo = torch.zeros_like(x) if two else None
+        call(x, lo_in, out, lo)
+        eng.check_device_status()
+        outs.append([o.view(n, Hq, d) for o in (out, lo) if o is not None])
+    for clean, got in zip(*outs):
+        assert bool(torch.isfinite(clean).all())
+        for r, h in bad:
+            assert bool(torch.isnan(got[r, h]).all())
+            got[r, h] = clean[r, h]
+        assert torch.equal(got, clean)
