@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         for (int s0 = 0; s0 < p.batch; s0 += 32) {
             int n = 0;
             if (s0 + lane < p.batch) {
-                const int P = max(p.seq_len[s0 + lane], 0);
+                const int P = positions(p.seq_len[s0 + lane], p.geom);
                 const int h = p.held_len ? min(max(p.held_len[s0 + lane], 0), P) / kPage : 0;
                 lens[s0 + lane] = P;
                 helds[s0 + lane] = h;

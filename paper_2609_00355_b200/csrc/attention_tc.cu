@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
     // context that no kernel of this pass writes, so the producer prefetches them before the wait as well.
     // A call by itself has no row-setup kernel before it: what it reads may have been written by the kernel just before.
     if (CACHE && !p.early) pdl_wait();
-    const int P = CACHE ? max(p.seq_len[s], 0) : p.seq_len[s];
+    const int P = CACHE ? positions(p.seq_len[s], p.geom) : p.seq_len[s];
     // keys any row of this tile sees: all of them, or, in a chain, those up to the tile's last node
     const int n_keys = P + (p.causal ? (min((qt + 1) * QT, PR) - 1) / G + 1 : p.T);
     // the pages that any row of this tile sees: all, or (CACHE) the entries of a list

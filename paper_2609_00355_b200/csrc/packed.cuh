@@ -63,6 +63,10 @@ __device__ __forceinline__ uint32_t half2_to_bf16(uint32_t h) {
 }  // namespace packed
 
 // ---- where a row looks: sliding window, sinks, trees (attention over a cache that is not read whole) ----------------
+// Positions of a sequence.  A length beyond the page table counts as one that fills it: the lists stay in 32 bits, and the page
+// behind the table's last entry, which the new rows need, is reported.
+__device__ __forceinline__ int positions(int seq_len, const KvGeom &g) { return min(max(seq_len, 0), g.max_pages_per_seq * kPage); }
+
 // The pages that any row of a tile sees, as one list: pages [0, head), then pages [next, end).
 struct PageList {
     int head, next, count;       // page of entry v: v < head ? v : v - head + next

@@ -962,3 +962,27 @@ def test_a_nan_in_a_query_stays_in_its_row(heads, two, kind, T, lens, window, si
             assert bool(torch.isnan(got[r, h]).all())
             got[r, h] = clean[r, h]
         assert torch.equal(got, clean)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, (8, 8, 128), HT])
+@pytest.mark.parametrize("kind,T,window,held", [("block", 1, 0, None), ("block", 1, 0, 64), ("block", 1, 500, 64), ("tree", 2, 0, 64), ("tree", 40, 0, None),
+                                                ("tree", 40, 300, 64), ("chain", 200, 0, 64), ("chain", 200, 100, None)])
+def test_lengths_beyond_the_page_table_are_reported(heads, kind, T, window, held):
+    """Up to the largest 32-bit length, where positions and page counts would pass 32 bits: the status word says so, and the
+    other sequences' rows are right."""
+    lens = [300, 2000, 40, 1500, 64]
+    cache = Cache(heads, lens, T, 96, held=held)
+    eng, (Hq, Hkv, d) = cache.eng, heads
+    cap = eng.pages_per_seq * PAGE
+    anc = torch.from_numpy(np.stack([anc_words(np.arange(T) - 1) for _ in lens])).cuda() if kind == "tree" else None
+    out = torch.empty_like(cache.q)
+    call = lambda: eng.glance_attention(0, cache.q, T, out, anc=anc, causal=kind == "chain", window=window, sinks=3)
+    for long in ((2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 1 - T, 2 ** 31 - 64), (1 << 30, cap), (cap - T + 1, cap - T + 1)):
+        eng.seq_len[1], eng.seq_len[3] = long
+        call()
+        assert eng.glance_poll_status() == -6
+        for s in (0, 2, 4):
+            see = visible(lens[s], T, kind, np.arange(T) - 1, window, 3)
+            ref, A = reference(cache.q.view(-1, T, Hq, d)[s].double(), cache.K[s], cache.V[s], see)
+            check(out.view(-1, T, Hq, d)[s], ref, A)
