@@ -25,6 +25,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "answers.h"
 #include "kernels.cuh"
 #include "packed.cuh"
 #include "tc_ptx.cuh"
@@ -1083,11 +1084,11 @@ cudaLaunchConfig_t few_config(cudaStream_t st) {
     return cfg;
 }
 
-// clusters of S CTAs that are resident at once (queried once per size; the kernel's attributes are set)
+// clusters of S CTAs that are resident at once (the kernel's attributes are set)
 template <int D, int NB, bool TWO>
-int few_clusters(int S) {
-    static int cache[kMaxCluster + 1] = {0};
-    if (cache[S] == 0) {
+int few_clusters(int dev, int S) {
+    static Answers<kMaxCluster + 1> answers;
+    return answers.get(dev, S, 1, [&] {
         cudaLaunchConfig_t cfg = few_config<D, NB>(nullptr);
         cfg.gridDim = dim3(S, 1, 1);
         cudaLaunchAttribute attr[1];
@@ -1098,23 +1099,17 @@ int few_clusters(int S) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, attn_few_kernel<D, NB, TWO>, &cfg) != cudaSuccess || n < 1) n = 1;
-        cache[S] = n;
-    }
-    return cache[S];
+        return cudaOccupancyMaxActiveClusters(&n, attn_few_kernel<D, NB, TWO>, &cfg) == cudaSuccess ? n : 0;
+    });
 }
 
 template <int D, int NB, bool TWO>
 cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, long long pages, cudaStream_t st) {
     using F = Few<D, NB>;
-    static bool once[kMaxDevices] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return cudaErrorInvalidDevice;
-    if (!once[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(attn_few_kernel<D, NB, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::TOTAL);
-        if (e != cudaSuccess) return e;
-        once[dev] = true;
-    }
+    static Answers<1> ready;
+    const int dev = current_device();
+    if (!ready.get(dev, 0, 0, [] { return cudaFuncSetAttribute(attn_few_kernel<D, NB, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::TOTAL) == cudaSuccess; }))
+        return cudaErrorInvalidDevice;
     const int items = p.Hkv * p.batch;
     // A cluster an item, whose CTAs add their parts through distributed shared memory in 1.5 us, where that costs a CTA no more
     // than kMorePages pages (0.4 us in 4 bits, 0.8 in bf16) beyond its share of the line; there the parts of an item meet in
@@ -1122,7 +1117,7 @@ cudaError_t launch_few(const AttnParams &p, const CUtensorMap &map_kv, long long
     AttnParams q = p;
     q.S = 0;
     for (int S = kMaxCluster; S > 1 && q.S == 0; S /= 2)
-        if (items <= few_clusters<D, NB, TWO>(S) && (pages + S - 1) / S <= (pages * items + 147) / 148 + kMorePages) q.S = S;
+        if (items <= few_clusters<D, NB, TWO>(dev, S) && (pages + S - 1) / S <= (pages * items + 147) / 148 + kMorePages) q.S = S;
     cudaLaunchConfig_t cfg = few_config<D, NB>(st);
     // (no more CTAs than pages)
     cfg.gridDim = dim3((unsigned)(q.S > 0 ? (long long)items * q.S : std::min<long long>(148, pages * items)), 1, 1);

@@ -42,6 +42,7 @@
 //   warps (64 rows over 8704 positions 49 us).
 #include <algorithm>
 
+#include "answers.h"
 #include "kernels.cuh"
 #include "packed.cuh"
 #include "tc_ptx.cuh"
@@ -948,14 +949,9 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
 
 template <int D, int CACHE>
 cudaError_t launch_d(const AttnParams &p, const CUtensorMap &map_kv, dim3 grid, cudaStream_t st) {
-    static bool once[kMaxDevices] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev >= kMaxDevices) return cudaErrorInvalidDevice;
-    if (!once[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, CACHE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
-        if (e != cudaSuccess) return e;
-        once[dev] = true;
-    }
+    static Answers<1> ready;
+    if (!ready.get(current_device(), 0, 0, [] { return cudaFuncSetAttribute(attn_tc_kernel<D, CACHE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL) == cudaSuccess; }))
+        return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(n_threads(CACHE), 1, 1);
@@ -973,13 +969,12 @@ cudaError_t launch_d(const AttnParams &p, const CUtensorMap &map_kv, dim3 grid, 
     return cudaLaunchKernelEx(&cfg, attn_tc_kernel<D, CACHE>, map_kv, p);
 }
 
-// largest number of co-resident clusters of `cs` CTAs of this kernel (queried once per cluster size; a CTA has the SM to
-// itself with or without CACHE)
+// largest number of co-resident clusters of `cs` CTAs of this kernel (a CTA has the SM to itself with or without CACHE)
 template <int D>
-int max_active_clusters(int cs) {
-    static int cache[MAX_SPLITS + 1] = {0};
-    if (cache[cs] == 0) {
-        cudaFuncSetAttribute(attn_tc_kernel<D, kWhole>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL);
+int max_active_clusters(int dev, int cs) {
+    static Answers<MAX_SPLITS + 1> answers;
+    return answers.get(dev, cs, std::max(148 / cs - 4, 1), [&] {
+        if (cudaFuncSetAttribute(attn_tc_kernel<D, kWhole>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::TOTAL) != cudaSuccess) return 0;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1, 1, cs);
         cfg.blockDim = dim3(n_threads(kWhole), 1, 1);
@@ -992,10 +987,8 @@ int max_active_clusters(int cs) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kWhole>, &cfg) != cudaSuccess || n < 1) n = 148 / cs - 4;
-        cache[cs] = n < 1 ? 1 : n;
-    }
-    return cache[cs];
+        return cudaOccupancyMaxActiveClusters(&n, attn_tc_kernel<D, kWhole>, &cfg) == cudaSuccess ? n : 0;
+    });
 }
 
 }  // namespace
@@ -1015,8 +1008,9 @@ int attention_tc_q_tiles(int T, int G) { return (T * G + QT - 1) / QT; }
 // Beyond one CTA per SM unsplit (a long prefill, many sequences) there is nothing to fill, and it stays unsplit.
 int attention_tc_splits(int T, int G, int Hkv, int batch, int d) {
     const int base = attention_tc_q_tiles(T, G) * Hkv * batch;
+    const int dev = current_device();
     for (int s = MAX_SPLITS; s > 1; --s) {
-        const int fit = d == 128 ? max_active_clusters<128>(s) : max_active_clusters<64>(s);
+        const int fit = d == 128 ? max_active_clusters<128>(dev, s) : max_active_clusters<64>(dev, s);
         if (base <= fit) return s;
     }
     return base <= 148 ? 2 : 1;
@@ -1038,7 +1032,8 @@ void attention_cache_splits(AttnParams &p, long long pages) {
     const int tiles = attention_tc_q_tiles(p.T, p.Hq / p.Hkv) * p.Hkv * p.batch;
     if (p.S < MAX_SPLITS || pages <= 12 * MAX_SPLITS) return;
     constexpr int S = 4;
-    const int fit = (p.d == 128 ? max_active_clusters<128>(S) : max_active_clusters<64>(S)) / tiles;
+    const int dev = current_device();
+    const int fit = (p.d == 128 ? max_active_clusters<128>(dev, S) : max_active_clusters<64>(dev, S)) / tiles;
     const int n = (int)std::min<long long>(fit, (pages + 4 * S - 1) / (4 * S));       // four pages a CTA at least
     if (n * S > p.S && (long long)tiles * n * QT <= kPartRows) {
         p.S = S;

@@ -19,7 +19,6 @@ constexpr int kPage = 64;        // tokens per KV page (an attention tile is two
 constexpr int kMaxTreeN = 128;   // verify rows per sequence, root included
 constexpr int kMaxTopk = 16;
 constexpr int kMaxBlock = 16;
-constexpr int kMaxDevices = 64;  // kernel attributes are set once a device
 
 // Paged KV pool geometry: element (layer, page, kv, kv_head, slot, dim), row-major.
 struct KvGeom {

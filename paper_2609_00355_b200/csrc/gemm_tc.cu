@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "answers.h"
 #include "gemm_epilogue.cuh"
 
 namespace glance {
@@ -612,12 +613,9 @@ EncodeTiledFn encode_fn() {
 template <int MODE>
 cudaError_t launch_mode(const TcGemmArgs &a, const CUtensorMap &mw, const CUtensorMap &mx, size_t smem, dim3 grid,
                         cudaStream_t st) {
-    static bool once = false;
-    if (!once) {
-        cudaError_t e = cudaFuncSetAttribute(gemm_tc_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
-        if (e != cudaSuccess) return e;
-        once = true;
-    }
+    static Answers<1> ready;
+    if (!ready.get(current_device(), 0, 0, [] { return cudaFuncSetAttribute(gemm_tc_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) == cudaSuccess; }))
+        return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(NTHR, 1, 1);
@@ -674,9 +672,9 @@ int tc_row_pad(int R) {
 // no device to ask.
 int tc_resident_clusters(int size) {
     static const int known[9] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
-    static int cache[9] = {0};
+    static Answers<9> answers;
     if (size < 1 || size > 8) return 0;
-    if (cache[size] == 0) {
+    return answers.get(current_device(), size, known[size], [&] {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1, size, 1);
         cfg.blockDim = dim3(NTHR, 1, 1);
@@ -689,14 +687,9 @@ int tc_resident_clusters(int size) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaFuncSetAttribute(gemm_tc_kernel<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, gemm_tc_kernel<3>, &cfg) != cudaSuccess || n < 1) {
-            (void)cudaGetLastError();
-            n = known[size];
-        }
-        cache[size] = n;
-    }
-    return cache[size];
+        return cudaFuncSetAttribute(gemm_tc_kernel<3>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) == cudaSuccess &&
+               cudaOccupancyMaxActiveClusters(&n, gemm_tc_kernel<3>, &cfg) == cudaSuccess ? n : 0;
+    });
 }
 
 // Split-K factor of a weight-streaming GEMM.  The splits of one tile form a thread-block cluster (<= 8 CTAs) that reduces them

@@ -30,6 +30,7 @@
 
 #include <algorithm>
 
+#include "answers.h"
 #include "gemm_epilogue.cuh"
 
 namespace glance {
@@ -689,12 +690,9 @@ __global__ void __launch_bounds__(NTHR, 1) gemm_wide_kernel(const __grid_constan
 
 template <int MODE>
 cudaError_t launch_mode(const TcGemmArgs &a, const CUtensorMap &mw, const CUtensorMap &mx, size_t smem, cudaStream_t st) {
-    static bool once = false;
-    if (!once) {
-        cudaError_t e = cudaFuncSetAttribute(gemm_wide_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem);
-        if (e != cudaSuccess) return e;
-        once = true;
-    }
+    static Answers<1> ready;
+    if (!ready.get(current_device(), 0, 0, [] { return cudaFuncSetAttribute(gemm_wide_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem) == cudaSuccess; }))
+        return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * a.wide_pairs, 1, 1);
     cfg.blockDim = dim3(NTHR, 1, 1);

@@ -1,5 +1,6 @@
 // Row setup kernels of the verify and draft passes (embedding gather, rotary table, paged row offsets, first
 // norm statistics) and the two-stage per-offset top-k + log-softmax of the draft pass.
+#include "answers.h"
 #include "gemm_tc.cuh"
 #include "kernels.cuh"
 #include "tc_ptx.cuh"
@@ -563,21 +564,15 @@ cudaLaunchConfig_t row_config(int ctas, int warps, int rows, cudaStream_t st, cu
     return cfg;
 }
 
-// rows whose clusters are resident at once (asked once per shape)
+// rows whose clusters are resident at once
 int resident_rows(int ctas, int warps) {
-    static int cache[2][kRowWarps + 1] = {{0}};
-    int &n = cache[ctas > 1 ? 1 : 0][warps];
-    if (n == 0) {
+    static Answers<2 * (kRowWarps + 1)> answers;
+    return answers.get(current_device(), (ctas > 1 ? kRowWarps + 1 : 0) + warps, ctas > 1 ? 15 : 148, [&] {
         cudaLaunchAttribute attr[1];
         const cudaLaunchConfig_t cfg = row_config(ctas, warps, 1, nullptr, attr);
-        int got = 0;
-        if (cudaOccupancyMaxActiveClusters(&got, topk_row_kernel, &cfg) != cudaSuccess || got < 1) {
-            (void)cudaGetLastError();
-            got = ctas > 1 ? 15 : 148;
-        }
-        n = got;
-    }
-    return n;
+        int n = 0;
+        return cudaOccupancyMaxActiveClusters(&n, topk_row_kernel, &cfg) == cudaSuccess ? n : 0;
+    });
 }
 
 }  // namespace

@@ -102,3 +102,71 @@ def test_topk_takes_one_launch_while_its_clusters_are_resident(lib, rows, spans,
     fn = lib._ZN6glance15topk_one_launchEiiiii
     fn.restype, fn.argtypes = C.c_bool, [C.c_int] * 5
     assert fn(rows, spans, warps, k, resident) is one
+
+
+ANSWERS = r"""
+#include "answers.h"
+#include <cstdio>
+#include <thread>
+#include <vector>
+
+static thread_local int device = 0;
+static thread_local bool no_device = false, error = false;
+extern "C" cudaError_t cudaGetDevice(int *d) {
+    if (no_device) { error = true; return cudaErrorNoDevice; }
+    *d = device;
+    return cudaSuccess;
+}
+extern "C" cudaError_t cudaGetLastError() { const bool was = error; error = false; return was ? cudaErrorUnknown : cudaSuccess; }
+
+static glance::Answers<9> answers;
+static int asked[3][9];                                  // (of devices 0..2, one thread)
+static int fit(int size, int fail = 0) {                 // "clusters of `size`": 100 a device and 10 a size
+    return answers.get(glance::current_device(), size, 7, [&] {
+        if (device < 3 && !no_device) ++asked[device][size];
+        if (fail) { error = true; return 0; }
+        return 100 * (device + 1) + 10 * size;
+    });
+}
+#define CHECK(x) if (!(x)) { std::printf("line %d: %s\n", __LINE__, #x); return 1; }
+
+int main() {
+    CHECK(fit(2, 1) == 7 && !error);                     // a failed question: the caller's default, no error left,
+    CHECK(fit(2) == 120 && asked[0][2] == 2);            // and it is asked again
+    CHECK(fit(2) == 120 && asked[0][2] == 2);            // once only
+    CHECK(fit(4) == 140 && asked[0][4] == 1);
+    device = 1;                                          // another device has answers of its own
+    CHECK(fit(2) == 220 && asked[1][2] == 1);
+    device = 0;
+    CHECK(fit(2) == 120 && asked[0][2] == 2);
+    no_device = true;                                    // none: asked every time, nothing kept
+    CHECK(fit(2, 1) == 7 && fit(2, 1) == 7 && !error);
+    no_device = false;
+    device = 1000;                                       // beyond the table: likewise
+    CHECK(fit(2) == 100120 && fit(2, 1) == 7);
+    std::vector<std::thread> threads;
+    std::vector<int> wrong(8, 0);
+    for (int t = 0; t < 8; ++t)
+        threads.emplace_back([t, &wrong] {
+            for (int i = 0; i < 20000; ++i) {
+                device = 3 + (i + t) % 61;
+                wrong[t] += fit(1 + i % 8) != 100 * (device + 1) + 10 * (1 + i % 8);
+            }
+        });
+    for (auto &t : threads) t.join();
+    for (int w : wrong) CHECK(w == 0);
+    return 0;
+}
+"""
+
+
+def test_answers_of_a_device(tmp_path):
+    """What launches ask once: per device, from any thread, a failure neither kept nor left as the thread's last error."""
+    import os
+    import subprocess
+    src, exe = tmp_path / "answers.cpp", tmp_path / "answers"
+    src.write_text(ANSWERS)
+    subprocess.run(["g++", "-std=c++17", "-pthread", "-O2", "-I", glance_build.CSRC, "-I", os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"),
+                    "-o", str(exe), str(src)], check=True, capture_output=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert res.returncode == 0, res.stdout + res.stderr
