@@ -118,6 +118,10 @@ typedef struct {
  * nearest to max|x| / 6 (448 at most, 0 where that rounds to 0); a value is held as the e2m1 value (0, 0.5, 1, 1.5, 2, 3, 4, 6
  * and their negatives) nearest to x / s and stands for s times it; ties go to the even code.  That product is exact in bf16.
  * 16 values with an infinity or a NaN among them are held as NaN.  4.5 bits a value: 3.56 times less than bf16.
+ * What that costs: normal values are off by 10 % of their root mean square (rms) down to an rms of 2^-5, by 11, 14 and 27 % at
+ * 2^-6, 2^-7 and 2^-8, since there is no scale beside s: groups with max|x| <= 6 x 2^-10 are held as zeros.  Attention over
+ * independent normal values, whose outputs are nearly all cancellation, is off by 15 to 27 % of the outputs' rms (10 % from V, the
+ * rest from K).
  * Positions [0, len[s]) of sequence s, whole pages, are read from `pool` in every target layer, later ones from kv_pool.
  * Only positions below seq_len are read here: of len[s], whole pages of it.  The block head's cache stays in bf16 and goes through
  * head_page_table, pages of a head_kv_pool of head_n_pages a layer; with it no pass looks at the entries of glance_seqs.page_table

@@ -12,13 +12,16 @@
 // takes 128 to 250 clocks of mma against 1400 (bf16) or 400 (4 bits) of its share of HBM.
 // 4-bit pages go from shared memory to registers in the order in which the mma wants them (16 consecutive d of a key per
 // lane; the contraction order is free as long as Q has the same), fp16: code x scale is exact there, and fp16 has the
-// conversion.  A row's queries are scaled by a power of two into fp16's range (exact); P is one fp16 term (half a step: 2^-11 relative), two
-// where the caller has two-term queries.  bf16 pages stay bf16: Q as it is, P in two bf16 terms (one would cost 2^-8).
+// conversion.  A row's queries are scaled by a power of two so that the largest lies in [1, 2): bf16 elements down to 2^-17 of it
+// keep all their bits, smaller ones are rounded to multiples of 2^-24.  P is one fp16 term (half a step: 2^-11 relative; outputs
+// then differ from those of an fp32 P by 7 to 9 x 10^-4 of their norm, half of what their own rounding to bf16 makes it, 1.7 x 10^-3),
+// two where the caller has two-term queries (16 rows over 4096-32768 positions 45 -> 53 us).  bf16 pages stay bf16: Q as it
+// is, P in two bf16 terms (one would cost 2^-8).
 // A row's reference is raised only when a score exceeds the largest so far by 2^8; sums and accumulators are fp32.
 // The warps' partial results meet in shared memory; an item that several CTAs share is finished by the one that comes last,
 // which adds the parts in line order, or by its cluster through distributed shared memory: results do not depend on timing.
 // Measured (us): 16 rows of 7 heads over 4096-32768 positions in 4 bits, 160 MB, 44.9 (3.6 TB/s); over 8192 positions in bf16,
-// 262 MB, 50.2 (5.2 TB/s); one row over 32801 positions in 4 bits 14.9, of which 5.5 are the merge of 37 parts; one row over a
+// 268 MB, 50.7 (5.3 TB/s); one row over 32801 positions in 4 bits 14.9, of which 5.5 are the merge of 37 parts; one row over a
 // window of 512 7.0.  In 4 bits the bound is the chain of a page in its warp (1300 clocks: first products 450, softmax 200,
 // second products 620), of which 12 warps keep three pages going; variants without the conversions, the mma or V's products
 // saved next to nothing.
@@ -42,9 +45,14 @@ constexpr int kMaxSeqs = 64;
 constexpr float kRaise = 8.f;                // log2 units a score may exceed its reference by
 constexpr float kHead = 7.f;                 // and the reference lies this far below the largest: fp16 probabilities reach from 2^15 down
                                              // to 2^-14 at full precision, 2^-21 of the largest
-constexpr int kLead4 = 24, kLead16 = 4;      // pages, in 4 bits and in bf16, that an item's end and the next one's start are worth (see the kernel)
+// Pages, in 4 bits and in bf16, that an item's end and the next one's start are worth (see the kernel).  Batches of 5, 16 and 40
+// ragged sequences at d 64 and 128: in 4 bits 8 places are 0 to 10 % slower than 24, 40 places 0 to 5 %; in bf16 none are 1 to 17 %
+// slower than 4, 12 places 3 % faster on average (1 % slower to 6 % faster).
+constexpr int kLead4 = 24, kLead16 = 4;
 constexpr int kMaxCluster = 8;
-constexpr int kMorePages = 3;                // pages a CTA may have more to be in a cluster (see launch_few)
+// Pages a CTA may have more to be in a cluster (see launch_few).  One to four rows over 600 to 1500 positions take 0.9 to 2.2 us
+// more with 0; with 8 single rows over 2100 to 4300 positions take 2.3 to 3.4 less, the others the same.
+constexpr int kMorePages = 3;
 
 // NB: blocks of 8 query rows.  As many teams as the registers of NB blocks' accumulators leave room for: a page's chain
 // (codes, first products, softmax, second products) is long, and only other warps' pages hide it.
@@ -573,7 +581,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
 #pragma unroll
                 for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(hi[e]));
                 top = warp_max(top);
-                // 2^-x brings the row into [1, 2); exact, and undone in the score's scale
+                // 2^-x brings the row's largest into [1, 2), which is undone in the score's scale
                 const int x = top > 0.f && top < INFINITY ? min(max(ilogbf(top), -100), 120) : 0;
                 const float down = exp2f((float)-x);
                 if (lane == 0) mask[r].scale16 = sl2 * exp2f((float)x);

@@ -24,8 +24,8 @@
 // instructions cold, and a CTA of a short context runs this code two or three times.
 // Measured per layer at the 7B widths against 64-key tiles with two threads a row and two S/P buffers a group, us: 128 rows
 // over 8704 positions 72 -> 46, 8 x 64 rows over 1024..4096 97 -> 71, 1280 rows of a prefill 97 -> 42, 64 rows over 1536
-// 17.8 -> 16.2, one row 15 -> 13.3; with the issuing warp going through its loop together the first two 43 and 64.  What is left of a long loop is the softmax warps (1.85 us per 128-key tile for
-// 1.05 of MMAs), of a short one the start and the merge.
+// 17.8 -> 16.2, one row 15 -> 13.3; with the issuing warp going through its loop together the first two 43 and 64.  What is left of
+// a long loop is the softmax warps (1.85 us per 128-key tile for 1.05 of MMAs), of a short one the start and the merge.
 // Warp roles: warp 0 = TMA producer, warp 1 = TMEM allocator + MMA issuer, warps 2..9 = softmax / epilogue.
 // The key splits of a tile form a thread-block cluster and are merged through distributed shared memory
 // (one asynchronous bulk copy per owner CTA, byte-counted on the owner's mbarrier).  Every mbarrier wait is
@@ -1026,6 +1026,8 @@ cudaError_t launch_attention_tc(const AttnParams &p, const CUtensorMap &map_kv, 
 // Splits and clusters a tile for a cache that is read in part or held in 4 bits.  As attention_tc_splits; where a launch has few
 // tiles and `pages` (as many as a row may see) leave a CTA more than 12 of them, every tile gets as many clusters of four as fit at
 // once, whose parts meet in global memory (3 to 4 us): 28 rows over 32000 positions 122 us with one cluster of eight a kv head, 33 so.
+// (Trees of 5 to 64 rows: with 6 pages as the border 0 to 1.3 us slower at 4500 positions and up to 1 faster at 6000; with 24, 0 to 10
+// slower at 8000 and 12000.  A plan is made for the longest sequence that the page table allows.)
 void attention_cache_splits(AttnParams &p, long long pages) {
     p.S = attention_tc_splits(p.T, p.Hq / p.Hkv, p.Hkv, p.batch, p.d);
     p.clusters = 1;
@@ -1034,7 +1036,7 @@ void attention_cache_splits(AttnParams &p, long long pages) {
     constexpr int S = 4;
     const int dev = current_device();
     const int fit = (p.d == 128 ? max_active_clusters<128>(dev, S) : max_active_clusters<64>(dev, S)) / tiles;
-    const int n = (int)std::min<long long>(fit, (pages + 4 * S - 1) / (4 * S));       // four pages a CTA at least
+    const int n = (int)std::min<long long>(fit, (pages + 4 * S - 1) / (4 * S));       // as many as take four pages a CTA
     if (n * S > p.S && (long long)tiles * n * QT <= kPartRows) {
         p.S = S;
         p.clusters = n;

@@ -5,8 +5,8 @@
 // lane takes one group of 16 values: one 32-byte load, the scale, eight conversions, one 8-byte store; the loads of a
 // thread's next tile are in flight while it converts, and the page numbers of the one after it.  The block that is the last to have read the lengths publishes the
 // new ones (nothing else in the launch reads what it writes), so nobody waits for the copies.
-// Measured: 8704 positions of 28 layers (4 kv heads, d 128), 640 MB each way: 110 us to pack, 113 back (5.7 TB/s); with a division a
-// value, 16-byte accesses and page numbers looked up when due 158 and 144.
+// Measured: 8704 positions of 28 layers (4 kv heads, d 128), 635 MB each way: 112 us to pack, 109 back (5.7 TB/s), 214 both in one
+// graph; with a division a value, 16-byte accesses and page numbers looked up when due 158 and 144.
 #include <cuda_fp8.h>
 
 #include "kernels.cuh"
@@ -26,7 +26,7 @@ constexpr int kMaxSeqs = 64;
 __device__ __forceinline__ int whole_pages(int n) { return max(n, 0) / kPage; }
 
 // e4m3 of a / 6 for a = max|x| >= 0.  a has eight significant bits, so a / 6 is a border of e4m3 exactly or at least 2^-9 of
-// itself away from one: rounding the product with 1 / 6 (off by 2^-23) to 12 bits makes borders exact again.
+// itself away from one: rounding the product with 1 / 6 (off by 2^-23) to 12 bits (Veltkamp's splitting) makes borders exact again.
 __device__ __forceinline__ uint32_t scale_code(float a) {
     const float q = fminf(a * (1.f / 6.f), 1024.f);      // (saturates at 448)
     const float wide = __fmul_rn(q, 4097.f), twelve = __fsub_rn(wide, __fsub_rn(wide, q));
