@@ -144,7 +144,8 @@ struct alignas(16) RowMask {
     uint32_t bits[4];
     int low;
     float scale16;               // score scale in log2 units for the fp16 queries of this row
-    int pad[2];
+    int sees;                    // whether it sees anything
+    int pad;
 };
 
 // The accumulators of a warp's 8 query rows from the 4-bit pages' order of d (lane g, register i: d = (D/8) g + i) to the mma's
@@ -531,14 +532,17 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
         for (int r = tid - (kWarps - 1) * 32; r >= 0 && r < 8 * NB; r += 32) {
             RowMask rm;
             rm.low = 0x7fffffff;                             // rows that do not exist see nothing
+            rm.sees = 0;
             rm.bits[0] = rm.bits[1] = rm.bits[2] = rm.bits[3] = 0;
             if (r < PR) {
                 const RowSight rs = row_sight(p.anc ? p.anc + (size_t)s * p.T * p.W : nullptr, p.causal, r / G, p.T, P, p.window, p.sinks);
                 rm.low = rs.low;
+                rm.sees = row_sees(rs, P, p.sinks);
                 rm.bits[0] = (uint32_t)rs.bits[0]; rm.bits[1] = (uint32_t)(rs.bits[0] >> 32);
                 rm.bits[2] = (uint32_t)rs.bits[1]; rm.bits[3] = (uint32_t)(rs.bits[1] >> 32);
             }
             mask[r].low = rm.low;
+            mask[r].sees = rm.sees;
 #pragma unroll
             for (int i = 0; i < 4; ++i) mask[r].bits[i] = rm.bits[i];
         }
@@ -904,7 +908,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                     sum_l[row] = L;
                 }
             } else if (parts == 1) {
-                const float inv = L > 0.f ? 1.f / L : 0.f;
+                const float inv = L > 0.f || mask[row].sees ? 1.f / L : 0.f;
                 const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
                 store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
             } else {
@@ -1035,7 +1039,7 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                         L += f * team_l[k * 8 * NB + row];
                         acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
                     }
-                    const float inv = L > 0.f ? 1.f / L : 0.f;
+                    const float inv = L > 0.f || mask[row].sees ? 1.f / L : 0.f;
                     const size_t off = ((size_t)(s * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
                     store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
                 }
@@ -1072,7 +1076,10 @@ __global__ void __launch_bounds__(Few<D, NB>::THREADS, 1) attn_few_kernel(const 
                     L += f * pl[k];
                     acc.x += f * a[k].x; acc.y += f * a[k].y; acc.z += f * a[k].z; acc.w += f * a[k].w;
                 }
-            const float inv = L > 0.f ? 1.f / L : 0.f;
+            int sees = 1;
+            if (!(L > 0.f))                                  // (the first CTA of a cluster has pages)
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(sees) : "r"(map_to_rank(smem_u32(&mask[row].sees), 0u)) : "memory");
+            const float inv = sees ? 1.f / L : 0.f;
             const size_t off = ((size_t)(sq * p.T + row / G) * p.Hq + kvh * G + row % G) * D + d0;
             store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
         }

@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
     unsigned char *sV = sK + NG * KV_BYTES;
     __shared__ AttnBars bars;
     __shared__ float red_m[NG][QT], red_l[NG][QT];        // the groups' reference maxima and row sums
+    __shared__ bool sees[CACHE ? QT : 1];                 // CACHE: whether a row sees anything
 
     unsigned long long *trace = (p.trace && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) ? p.trace : nullptr;
     if (trace && threadIdx.x == 0) trace[0] = global_ns();
@@ -549,6 +550,7 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
             anc0 = rs.bits[0];
             anc1 = rs.bits[1];
             low = rs.low;
+            if (grp == 0) sees[row] = !p.anc || row_sees(rs, P, p.sinks);      // (a chain's or a block's row sees itself)
         } else if (p.anc && !p.causal) {
             const uint64_t *a = p.anc + ((size_t)s * p.T + node) * p.W;
             anc0 = a[0];
@@ -740,9 +742,11 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
         ok = __all_sync(0xffffffffu, ok);
         if (trace && threadIdx.x == 64) trace[7] = global_ns();
         // ---------------- epilogue ----------------
+        // 1 / the sum of the weights of a row of the tile; CACHE: 0 where the row sees nothing
+        auto inverse = [&](float sum, int r) { return !CACHE || sum > 0.f || sees[r] ? 1.f / sum : 0.f; };
         constexpr int OC = D / ECG;                       // output columns of a thread
         if (p.S == 1 && (!CACHE || p.clusters == 1)) {
-            const float inv = CACHE && l_row == 0.f ? 0.f : 1.f / l_row;      // a row that sees nothing
+            const float inv = inverse(l_row, row);
             const bool aligned = (((uintptr_t)p.out | (uintptr_t)p.out_lo) & 15) == 0;     // (rows start on multiples of 128 bytes)
             const size_t off = ((size_t)(s * p.T + node) * p.Hq + kvh * G + g) * D + grp * OC;
 #pragma unroll 1
@@ -862,8 +866,8 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                         continue;
                     }
                 }
-                const float inv = CACHE && den == 0.f ? 0.f : 1.f / den;
                 const int prr = qt * QT + row_lo + lr;
+                const float inv = inverse(den, row_lo + lr);
                 const size_t off = ((size_t)(s * p.T + prr / G) * p.Hq + kvh * G + prr % G) * D;
                 store_two_term(p.out + off + c0, p.out_lo ? p.out_lo + off + c0 : nullptr,
                                make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
@@ -918,8 +922,8 @@ __global__ void __launch_bounds__(n_threads(CACHE), 1) attn_tc_kernel(const __gr
                             }
                             M = M2;
                         }
-                        const float inv = den == 0.f ? 0.f : 1.f / den;
                         const int prr = qt * QT + row_lo + lr;
+                        const float inv = inverse(den, row_lo + lr);
                         const size_t off = ((size_t)(s * p.T + prr / G) * p.Hq + kvh * G + prr % G) * D + c0;
                         store_two_term(p.out + off, p.out_lo ? p.out_lo + off : nullptr, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
                     }

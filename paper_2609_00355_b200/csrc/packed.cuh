@@ -133,4 +133,10 @@ __device__ inline RowSight row_sight(const uint64_t *anc, int causal, int node, 
     return r;
 }
 
+// Whether a row sees anything.  One that does and has no weight has scores that are all -inf (an infinite query's): its outputs are
+// NaN, the definition's 0 / 0, where those of a row that sees nothing are zeros.
+__device__ __forceinline__ bool row_sees(const RowSight &r, int P, int sinks) {
+    return (r.bits[0] | r.bits[1]) != 0ull || (P > 0 && (sinks > 0 || r.low < P));
+}
+
 }  // namespace glance

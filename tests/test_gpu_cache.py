@@ -986,3 +986,42 @@ def test_lengths_beyond_the_page_table_are_reported(heads, kind, T, window, held
             see = visible(lens[s], T, kind, np.arange(T) - 1, window, 3)
             ref, A = reference(cache.q.view(-1, T, Hq, d)[s].double(), cache.K[s], cache.V[s], see)
             check(out.view(-1, T, Hq, d)[s], ref, A)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [H7, HS])
+@pytest.mark.parametrize("two", [False, True])
+@pytest.mark.parametrize("kind,T,lens,window,sinks,held", [
+    ("block", 1, [1536], 512, 4, None), ("block", 1, [1536], 512, 4, 64), ("block", 1, [0, 64, 700], 1, 0, 64), ("block", 2, [0, 300], 0, 0, 64),
+    ("block", 1, [9000], 0, 0, 64), ("block", 1, [500, 6000, 100], 0, 0, 64), ("tree", 64, [1536], 512, 4, None), ("tree", 40, [700, 64], 0, 0, 64),
+    ("tree", 8, [9000], 0, 0, 64), ("chain", 200, [300], 100, 5, None), ("chain", 1300, [70], 0, 0, 0)])
+def test_an_infinite_query_gives_nan(heads, two, kind, T, lens, window, sinks, held):
+    """All its scores are -inf where its sign differs from every key's: 0 / 0 by the definition, not a row that sees nothing."""
+    cache = Cache(heads, lens, T, 82)
+    eng, (Hq, Hkv, d) = cache.eng, heads
+    eng.kv_pool[:, :, 0, :, :, 3] = -1 - eng.kv_pool[:, :, 0, :, :, 3].abs()
+    if held is not None:
+        from paper_2609_00355_b200.binding import PackedCache
+        eng.glance_set_packed(PackedCache(eng))
+        eng.glance_pack_cache(keep=held)
+    rng = np.random.default_rng(2)
+    anc = torch.from_numpy(np.stack([anc_words(np.arange(T) - 1) for _ in lens])).cuda() if kind == "tree" else None
+    n = len(lens) * T
+    bad = sorted({(int(rng.integers(0, n)), int(rng.integers(0, Hq))): (-1) ** i for i in range(4)}.items())
+    q = cache.q.clone()
+    for (r, h), sign in bad:
+        q[r, h * d + 3] = sign * math.inf
+    outs = []
+    for x in (cache.q, q):
+        out = torch.zeros_like(x)
+        lo = torch.zeros_like(x) if two else None
+        eng.glance_attention(0, x, T, out, anc=anc, causal=kind == "chain", window=window, sinks=sinks,
+                             q_lo=(cache.q * 2.0 ** -9).contiguous() if two else None, out_lo=lo)
+        eng.check_device_status()
+        outs.append([o.view(n, Hq, d) for o in (out, lo) if o is not None])
+    for clean, got in zip(*outs):
+        assert bool(torch.isfinite(clean).all())
+        for (r, h), _ in bad:
+            assert bool(torch.isnan(got[r, h]).all())
+            got[r, h] = clean[r, h]
+        assert torch.equal(got, clean)
