@@ -258,10 +258,10 @@ int32_t glance_unpack_cache(glance_ctx *ctx, const glance_seqs *seqs, const int3
  * the number of nodes in its set without itself; causal != 0: rows 0..i (a chain: prefill; anc must be NULL), neither: all T rows
  * (a block).  In a chain or a block row i stands at seq_len + i.  window and sinks limit all of them as in glance_set_window
  * (whose setting does not apply here; within a set the distance of two nodes is the number of its nodes behind the nearer
- * one), and positions held in 4 bits are read from the registered pool.  A row that sees nothing gets zeros, one with a
- * NaN or an infinity in its query that sees something NaN.  Cache rows
- * from seq_len + T on, and committed ones that a row at position seq_len would not see, may hold anything; values elsewhere
- * have to be finite even where only some rows see them.  T <= 128 with anc or as a block; a chain may be as long as the page table allows.
+ * one), and positions held in 4 bits are read from the registered pool.  A row that sees nothing gets zeros; one that sees
+ * something and has a NaN or an infinity in its query gets NaN.  Cache rows from seq_len + T on, and committed ones that a row at
+ * position seq_len would not see, may hold anything; values elsewhere have to be finite even where only some rows see them.
+ * T <= 128 with anc or as a block; a chain may be as long as the page table allows.
  * seq_len[s] + T positions have to fit the page table and its entries the pools: GLANCE_E_BOUNDS in the status word otherwise,
  * and that sequence's rows are undefined.  q_lo and out_lo: second bf16 terms as in glance_debug_attention, or NULL. */
 int32_t glance_attention(glance_ctx *ctx, const glance_seqs *seqs, int32_t layer, const void *q, const void *q_lo,
