@@ -247,7 +247,7 @@ int32_t glance_pack_cache(glance_ctx *ctx, const glance_seqs *seqs, int32_t keep
 
 /* The way back: len[s] falls to new_len[s] rounded down to whole pages (device [batch]; larger values change nothing), and
  * the values that the pages from there on stand for are written to the pages of seqs->kv_pool.  Where a page due has no place
- * (as above), len[s] falls only to behind the last such page, with GLANCE_E_BOUNDS in the status word.  Before a truncation into
+ * (as above), len[s] falls only to behind the last such page, with GLANCE_E_BOUNDS in the status word (the others are written).  Before a truncation into
  * the 4-bit part, or to look at what is held (with a kv_pool of the caller's own in *seqs).  GLANCE_E_STATE without a pool. */
 int32_t glance_unpack_cache(glance_ctx *ctx, const glance_seqs *seqs, const int32_t *new_len);
 

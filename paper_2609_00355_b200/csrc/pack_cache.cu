@@ -3,8 +3,8 @@
 // HBM-bound: 2 bytes of a value are read and 9/16 of one written, or the other way round.  One wave of blocks takes the tiles
 // (layer, page, kv head, K|V) in turn; which pages are due is worked out from the device-resident lengths by every block.  A
 // lane takes one group of 16 values: one 32-byte load, the scale, eight conversions, one 8-byte store; the loads of a
-// thread's next tile are in flight while it converts, and the page numbers of the one after it.  The block that is the last to have read the lengths publishes the
-// new ones (nothing else in the launch reads what it writes), so nobody waits for the copies.
+// thread's next tile are in flight while it converts, and the page numbers of the one after it.  The block that is the last to
+// have read the lengths publishes the new ones (nothing else in the launch reads what it writes), so nobody waits for the copies.
 // Measured: 8704 positions of 28 layers (4 kv heads, d 128), 635 MB each way: 112 us to pack, 109 back (5.7 TB/s), 214 both in one
 // graph; with a division a value, 16-byte accesses and page numbers looked up when due 158 and 144.
 #include <cuda_fp8.h>
@@ -97,70 +97,42 @@ __device__ __forceinline__ void unpack_group(uint2 c, uint32_t scale, uint4 (&v)
 template <int D, bool BACK>
 __global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(PackParams p) {
     constexpr int GROUPS = Tile<D>::GROUPS;
-    __shared__ int sh_first[kMaxSeqs], sh_upto[kMaxSeqs + 1], sh_len[kMaxSeqs];      // first page due, pages due up to here, new length
-    __shared__ int sh_stop[kMaxSeqs];                    // first page without a place (back: one past the last)
+    __shared__ int sh_first[kMaxSeqs], sh_upto[kMaxSeqs + 1], sh_len[kMaxSeqs];      // first page due, pages due up to here, new length in pages
+    __shared__ int sh_ticket;
     const int t = threadIdx.x, cap = p.geom.max_pages_per_seq;
-    int lo = 0, hi = 0;                                  // thread t: sequence t's pages due are lo .. hi - 1
-    auto due = [&]() {
-        if (t < p.batch) {
-            sh_first[t] = lo;
-            sh_upto[t + 1] = hi - lo;
-            sh_len[t] = (BACK ? lo : hi) * kPage;
-        }
-        __syncthreads();
-        if (t < 32) {                                    // prefix sums
-            int run = 0;
-            for (int s0 = 0; s0 < p.batch; s0 += 32) {
-                int n = s0 + t < p.batch ? sh_upto[s0 + t + 1] : 0;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int v = __shfl_up_sync(0xffffffffu, n, o);
-                    if (t >= o) n += v;
-                }
-                if (s0 + t < p.batch) sh_upto[s0 + t + 1] = run + n;
-                run += __shfl_sync(0xffffffffu, n, 31);
-            }
-            if (t == 0) sh_upto[0] = 0;
-        }
-        __syncthreads();
-    };
     if (t < p.batch) {
         const int seen = max(p.seq_len[t], 0);
         const int have = min(min(whole_pages(p.len[t]), whole_pages(seen)), cap);      // a length beyond seq_len counts for nothing
+        int lo, hi;
         if (BACK) {
             lo = min(whole_pages(p.new_len[t]), have);
             hi = have;
+            sh_len[t] = lo;
         } else {
             lo = have;
             hi = max(min(whole_pages(seen - p.keep), cap), have);
+            sh_len[t] = hi;
             if (whole_pages(seen) > cap) set_status(p.status, GLANCE_E_CAPACITY);
         }
-        sh_stop[t] = BACK ? 0 : cap;
+        sh_first[t] = lo;
+        sh_upto[t + 1] = hi - lo;
     }
-    due();
-    // A page that has no place in one of the pools cannot move, and positions held in 4 bits are a prefix: a length rises to the
-    // first such page only, and falls to behind the last one.  Every block looks at every entry due, 8 bytes a page for at least
-    // 20 KB that move, which takes 0.3 to 0.6 us a launch (beside the first tile's loads 0.2, and then the loop ran 1 to
-    // 2 % slower).
-    bool lost = false;
-    for (int pg = t, s = 0; pg < sh_upto[p.batch]; pg += kPackThreads) {
-        while (sh_upto[s + 1] <= pg) ++s;
-        const int at = sh_first[s] + pg - sh_upto[s];
-        const size_t entry = (size_t)s * cap + at;
-        const int from = p.page_table[entry], at4 = p.page_table4[entry];
-        if (from >= 0 && from < p.geom.n_pages && at4 >= 0 && at4 < p.n_pages4) continue;
-        lost = true;
-        if (BACK) atomicMax(&sh_stop[s], at + 1);
-        else atomicMin(&sh_stop[s], at);
-    }
-    if (__syncthreads_or(lost)) {
-        if (lost) set_status(p.status, GLANCE_E_BOUNDS);
-        if (t < p.batch) {
-            if (BACK) lo = max(lo, sh_stop[t]);
-            else hi = min(hi, sh_stop[t]);
+    __syncthreads();
+    if (t < 32) {                                        // prefix sums
+        int run = 0;
+        for (int s0 = 0; s0 < p.batch; s0 += 32) {
+            int n = s0 + t < p.batch ? sh_upto[s0 + t + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, n, o);
+                if (t >= o) n += v;
+            }
+            if (s0 + t < p.batch) sh_upto[s0 + t + 1] = run + n;
+            run += __shfl_sync(0xffffffffu, n, 31);
         }
-        due();
+        if (t == 0) sh_upto[0] = 0;
     }
+    __syncthreads();
     // counted in: this block has read the lengths (the answer is looked at when its tiles are done)
     int ticket = 0;
     if (t == 0) ticket = atomicAdd(p.counter, 1);
@@ -175,6 +147,7 @@ __global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(PackPar
         bf16 *rows;              // nullptr: nothing to move
         unsigned char *tile;
     };
+    auto placed = [&](int from, int at4) { return from >= 0 && from < p.geom.n_pages && at4 >= 0 && at4 < p.n_pages4; };
     auto find = [&](unsigned it) {
         Item r{nullptr, nullptr};
         if (it >= items) return r;
@@ -183,7 +156,11 @@ __global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(PackPar
         int s = 0;
         while ((unsigned)sh_upto[s + 1] <= pg) ++s;
         const size_t entry = (size_t)s * cap + sh_first[s] + (int)pg - sh_upto[s];
-        const int from = p.page_table[entry], at4 = p.page_table4[entry];      // (places: see above)
+        const int from = p.page_table[entry], at4 = p.page_table4[entry];
+        if (!placed(from, at4)) {
+            if (t == 0) set_status(p.status, GLANCE_E_BOUNDS);
+            return r;
+        }
         r.rows = p.kv_pool + (size_t)layer * p.geom.layer_stride() + p.geom.row(from, kv, head, 0);
         r.tile = p.pool4 + layer * layer4 + ((size_t)at4 * p.geom.n_kv_heads + head) * Tile<D>::BYTES + kv * Tile<D>::HALF;
         return r;
@@ -209,6 +186,18 @@ __global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(PackPar
     Data now;
     Item item = find(blockIdx.x);
     load(item, now);
+    // A page that has no place in one of the pools stays, and positions held in 4 bits are a prefix: a length rises to the first such
+    // page only, and falls to behind the last one (what moves on the far side is not read there).  Every block looks at every entry
+    // due while its first tile is on its way, 8 bytes a page for at least 20 KB that move: no time that was measured with one page
+    // or many, 1 % with 84 pages of a small model; before the first tile's loads it took 0.5 us a launch.
+    for (int pg = t, s = 0; pg < (int)pages; pg += kPackThreads) {
+        while (sh_upto[s + 1] <= pg) ++s;
+        const int at = sh_first[s] + pg - sh_upto[s];
+        const size_t entry = (size_t)s * cap + at;
+        if (placed(p.page_table[entry], p.page_table4[entry])) continue;
+        if (BACK) atomicMax(&sh_len[s], at + 1);
+        else atomicMin(&sh_len[s], at);
+    }
     Item following = find(blockIdx.x + gridDim.x);
     for (unsigned it = blockIdx.x; it < items; it += gridDim.x) {
         Data next;
@@ -239,9 +228,11 @@ __global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(PackPar
         now = next;
     }
     // the block that counted itself in last publishes the new lengths: every block has read the old ones
-    if (t < 32 && __shfl_sync(0xffffffffu, ticket, 0) == (int)gridDim.x - 1) {
+    if (t == 0) sh_ticket = ticket;
+    __syncthreads();
+    if (sh_ticket == (int)gridDim.x - 1) {
         if (t == 0) *p.counter = 0;                      // for the next launch
-        for (int s = t; s < p.batch; s += 32) p.len[s] = sh_len[s];
+        if (t < p.batch) p.len[t] = sh_len[t] * kPage;
     }
 }
 

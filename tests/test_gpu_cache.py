@@ -898,7 +898,7 @@ def test_packing_stops_before_a_page_without_a_place(heads, layers):
 @pytest.mark.gpu
 @pytest.mark.parametrize("heads,layers", [(H7, 2), (HS, 3)])
 def test_unpacking_stops_behind_a_page_without_a_place(heads, layers):
-    """The way back: a length does not fall below a page that could not be written, and the pages behind it are."""
+    """The way back: a length does not fall below a page that could not be written; the others due are written, no more."""
     from paper_2609_00355_b200.binding import PackedCache
     lens, T = [700, 300, 130, 1000], 2
     cache = Cache(heads, lens, T, 92, layers=layers)
@@ -909,16 +909,16 @@ def test_unpacking_stops_behind_a_page_without_a_place(heads, layers):
     eng.check_device_status()
     K, V = [k.clone() for k in cache.K], [v.clone() for v in cache.V]
     table, own = eng.page_table.clone(), packed.page_table.clone()
-    eng.page_table[0, 2] = -1                            # due from page 1 on: pages 6.. come back
+    eng.page_table[0, 2] = -1                            # due from page 1 on: pages 6.. are back
     eng.page_table[0, 5] = eng.n_pages
     eng.page_table[1, 0] = -1                            # not due
-    packed.page_table[3, 14] = -1                        # the last one held has no place to be read from: nothing comes back
+    packed.page_table[3, 14] = -1                        # the last one held has no place to be read from: nothing is back
     back = torch.full_like(x, 3.0)
     eng.glance_unpack_cache(torch.tensor([64, 128, 1 << 20, 0], dtype=torch.int32, device="cuda"), kv_pool=back)
     assert eng.glance_poll_status() == -6
     assert packed.len.tolist() == [6 * 64, 128, 128, 15 * 64]
     ref = torch.full(x.shape, 3.0, dtype=torch.float64, device="cuda")
-    for s, pages in ((0, range(6, 10)), (1, (2, 3))):
+    for s, pages in ((0, (1, 3, 4, 6, 7, 8, 9)), (1, (2, 3)), (3, range(14))):
         for p in pages:
             ref[:, int(table[s, p])] = held_values(x[:, int(table[s, p])])
     assert torch.equal(back.double(), ref)
