@@ -206,6 +206,8 @@ class PackedCache:
     """
 
     def __init__(self, eng: "Engine", n_pages: Optional[int] = None, head_page_table: Optional[torch.Tensor] = None):
+        assert head_page_table is None or (head_page_table.dtype is torch.int32 and head_page_table.shape == eng.page_table.shape)
+        assert head_page_table is None or head_page_table.get_device() == eng.device_index, "the engine's device"
         self.n_pages = eng.n_pages if n_pages is None else n_pages
         nbytes = eng.lib.glance_packed_bytes(C.byref(eng.ccfg), self.n_pages)
         if nbytes == 0:
@@ -214,7 +216,6 @@ class PackedCache:
         ids = torch.arange(eng.batch * eng.pages_per_seq, dtype=torch.int32, device=eng.device).view(eng.batch, -1)
         self.page_table = torch.where(ids < self.n_pages, ids, -1)
         self.pool = torch.zeros(nbytes, dtype=torch.uint8, device=eng.device)
-        assert head_page_table is None or (head_page_table.dtype is torch.int32 and head_page_table.shape == eng.page_table.shape)
         self.head_page_table = head_page_table
         self.c = Packed(self.n_pages, _ptr(self.len), _ptr(self.page_table), _ptr(self.pool), _ptr(head_page_table),
                         0 if head_page_table is None else eng.n_pages)
@@ -233,6 +234,7 @@ class Engine:
         self.batch = batch
         self.device = target["embed"].device
         assert self.device.type == "cuda", "the library runs on a CUDA device only"
+        self.device_index = target["embed"].get_device()
         self.stream = stream
         page = cfg.page_size
         max_len = max_len or (cfg.ctx + cfg.rounds * cfg.block_B + 2 * cfg.tree_N + page)
@@ -377,6 +379,7 @@ class Engine:
     def glance_unpack_cache(self, new_len: torch.Tensor, kv_pool: Optional[torch.Tensor] = None):
         """Pages from new_len [batch] (int32, device) on back to bf16: into the engine's pool, or into another of its shape."""
         assert new_len.dtype is torch.int32 and new_len.numel() == self.batch, "new_len: int32, one a sequence"
+        assert new_len.get_device() == self.device_index and (kv_pool is None or kv_pool.get_device() == self.device_index), "the engine's device"
         if kv_pool is None:
             _check(self.lib.glance_unpack_cache(self.ctx, C.byref(self.seqs), _ptr(new_len)), "glance_unpack_cache")
             return
@@ -392,9 +395,12 @@ class Engine:
                          out_lo: Optional[torch.Tensor] = None):
         """Attention of T rows a sequence over layer `layer`'s cache (window, sinks, 4-bit pages): see glance.h."""
         n = self.batch * T * self.ccfg.n_q_heads * self.ccfg.head_dim
+        dev = self.device_index
         for x in (q, out) if q_lo is None and out_lo is None else (q, out, q_lo, out_lo):
             assert x is None or (x.dtype is torch.bfloat16 and x.numel() == n), "bf16 tensors of batch * T rows"
+            assert x is None or x.get_device() == dev, "the engine's device"
         assert anc is None or (anc.dtype is torch.int64 and anc.numel() == self.batch * T * ((T + 63) // 64)), "anc: 64-bit words"
+        assert anc is None or anc.get_device() == dev, "the engine's device"
         _check(self.lib.glance_attention(self.ctx, C.byref(self.seqs), layer, _ptr(q), _ptr(q_lo), _ptr(anc), T, 1 if causal else 0,
                                          window, sinks, _ptr(out), _ptr(out_lo)), "glance_attention")
 

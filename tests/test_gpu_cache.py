@@ -1025,3 +1025,34 @@ def test_an_infinite_query_gives_nan(heads, two, kind, T, lens, window, sinks, h
             assert bool(torch.isnan(got[r, h]).all())
             got[r, h] = clean[r, h]
         assert torch.equal(got, clean)
+
+
+def test_tensors_of_another_device_are_refused():
+    """A pointer into another GPU's memory would fault on this one: refused before the library is called."""
+    from types import SimpleNamespace
+
+    from paper_2609_00355_b200.binding import Engine, PackedCache
+
+    def tensor(dtype, n, index=0):
+        return SimpleNamespace(dtype=dtype, numel=lambda: n, shape=(1, n), get_device=lambda: index, is_cuda=True, is_contiguous=lambda: True,
+                               data_ptr=lambda: 1 << 20)
+    called = []
+    eng = SimpleNamespace(batch=1, device_index=0, ctx=None, seqs=C.c_int(), ccfg=SimpleNamespace(n_q_heads=4, head_dim=64),
+                          kv_pool=tensor(torch.bfloat16, 8),
+                          lib=SimpleNamespace(glance_attention=lambda *a: called.append(a) or 0, glance_unpack_cache=lambda *a: called.append(a) or 0))
+    row = lambda index=0: tensor(torch.bfloat16, 256, index)
+    Engine.glance_attention(eng, 0, row(), 1, row(), anc=tensor(torch.int64, 1), q_lo=row(), out_lo=row())
+    Engine.glance_unpack_cache(eng, tensor(torch.int32, 1))
+    assert len(called) == 2
+    for args, kw in (((row(1), row()), {}), ((row(), row(1)), {}), ((row(), row()), dict(anc=tensor(torch.int64, 1, 1))),
+                     ((row(), row()), dict(q_lo=row(1))), ((row(), row()), dict(out_lo=row(1)))):
+        with pytest.raises(AssertionError, match="the engine's device"):
+            Engine.glance_attention(eng, 0, args[0], 1, args[1], **kw)
+    with pytest.raises(AssertionError, match="the engine's device"):
+        Engine.glance_unpack_cache(eng, tensor(torch.int32, 1, 1))
+    with pytest.raises(AssertionError, match="the engine's device"):
+        Engine.glance_unpack_cache(eng, tensor(torch.int32, 1), kv_pool=tensor(torch.bfloat16, 8, 1))
+    eng.page_table = tensor(torch.int32, 3)
+    with pytest.raises(AssertionError, match="the engine's device"):
+        PackedCache(eng, head_page_table=tensor(torch.int32, 3, 1))
+    assert len(called) == 2
