@@ -369,6 +369,10 @@ class Engine:
 
     def glance_set_packed(self, packed: Optional[PackedCache]):
         """Registers (and keeps alive) a 4-bit pool for the target's layers, or goes back to the bf16 pool alone."""
+        if packed is not None:
+            fits = packed.page_table.shape == self.page_table.shape and packed.pool.get_device() == self.device_index
+            if not fits or packed.pool.numel() != self.lib.glance_packed_bytes(C.byref(self.ccfg), packed.n_pages):
+                raise GlanceError("glance_set_packed: a pool made for another engine")
         _check(self.lib.glance_set_packed(self.ctx, None if packed is None else C.byref(packed.c)), "glance_set_packed")
         self.packed = packed
 

@@ -1056,3 +1056,32 @@ def test_tensors_of_another_device_are_refused():
     with pytest.raises(AssertionError, match="the engine's device"):
         PackedCache(eng, head_page_table=tensor(torch.int32, 3, 1))
     assert len(called) == 2
+
+
+def test_a_pool_made_for_another_engine_is_refused():
+    """Its page table or its pages have another size, or it lies on another device: the kernels would read beyond it."""
+    from types import SimpleNamespace
+
+    from paper_2609_00355_b200 import binding
+    from paper_2609_00355_b200 import build as glance_build
+    glance_build.build()
+    lib = binding.load_library()
+    called = []
+
+    def engine(name, pages):
+        return SimpleNamespace(ccfg=binding.make_config(synth.CONFIGS[name], 2, pages), page_table=torch.zeros(2, pages), device_index=0, ctx=None,
+                               lib=SimpleNamespace(glance_packed_bytes=lib.glance_packed_bytes, glance_set_packed=lambda *a: called.append(a) or 0))
+
+    def packed(eng, n_pages, index=0):
+        nbytes = lib.glance_packed_bytes(C.byref(eng.ccfg), n_pages)
+        return SimpleNamespace(n_pages=n_pages, page_table=eng.page_table, pool=SimpleNamespace(numel=lambda: nbytes, get_device=lambda: index), c=binding.Packed())
+    small, longer, wide = engine("small", 9), engine("small", 10), engine("7b", 9)
+    fits = packed(small, 5)
+    binding.Engine.glance_set_packed(small, fits)
+    assert small.packed is fits and len(called) == 1
+    for other in (packed(longer, 5), packed(wide, 5), packed(small, 5, index=1)):
+        with pytest.raises(binding.GlanceError, match="another engine"):
+            binding.Engine.glance_set_packed(small, other)
+    assert small.packed is fits and len(called) == 1
+    binding.Engine.glance_set_packed(small, None)
+    assert small.packed is None and len(called) == 2
